@@ -16,6 +16,10 @@
  *   map_prune       all of the above fused, plus the gather of the kept rows
  *                   and of their positional indices
  *
+ * Behind it, the language model's side of a pruned sequence: a decoder layer's
+ * prefill (map_decoder_layer) and the key/value cache that later tokens read
+ * (map_qk_norm_rope, map_cache_append, map_cache_read, map_cache_attention).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * Pointers.  Every tensor argument is a DEVICE pointer into memory the caller
@@ -343,6 +347,127 @@ map_status map_decoder_layer(const map_decoder_weights* w, map_dtype dt, int B, 
                              const int32_t* pos, const int32_t* seq_off_host, void* Y,
                              void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------ key/value cache
+ * What a pruned sequence leaves behind for its later tokens: the keys and
+ * values of its kept visual tokens, of its question and of every token since.
+ * A step of one layer is
+ *   map_qk_norm_rope     the new rows' queries and keys, turned by position;
+ *   map_cache_append     their keys and values into the sequence's pages;
+ *   map_cache_attention  their attention over everything in those pages,
+ * for whole prompts and for single tokens alike; map_cache_read takes cached
+ * rows out again.  Offsets (seq_off_host, [B + 1], host) start at 0 and do not
+ * decrease: sequence b's new rows are rows seq_off[b] .. seq_off[b+1]-1, none
+ * of them if the two are equal; rows from seq_off[B] on are neither read nor
+ * written.  Row strides (ld*) count elements: heads lie next to each other in
+ * a row, rows ld apart, so that parts of a wider product (a [R][3 d] qkv) serve
+ * as they are.  Row pointers are 16-byte aligned and strides a multiple of 16
+ * bytes.  Limits: 1 <= B <= MAP_CACHE_MAX_BATCH, at most
+ * MAP_CACHE_MAX_ROWS rows a call. */
+#define MAP_CACHE_MAX_BATCH 256
+#define MAP_CACHE_MAX_ROWS (1 << 20)
+
+/* Rotary positions of head_dim values a head (64 or 128), the first rot_dim of
+ * them rotated (a multiple of 16, at most head_dim): pair i, (i, i + rot_dim/2),
+ * by pos[axis(i)][r] * theta^(-2i / rot_dim).  Axis a (of n_axes, at most 4)
+ * turns sections[a] pairs, rot_dim / 2 in all: interleaved == 0 gives axis 0
+ * the first sections[0] pairs, axis 1 the next ones and so on; otherwise the
+ * axes take one pair each in turn, those that have theirs left out.  One axis
+ * is the rotation of text; three are time, height and width of image and video
+ * tokens.  eps is the norms' (below). */
+typedef struct {
+  int32_t head_dim, rot_dim, n_axes, interleaved;
+  int32_t sections[4];
+  float theta, eps;
+} map_rope;
+
+/* map_qk_norm_rope -- one pass over the query and key heads of R rows:
+ *   y = x / sqrt(mean(x^2) + eps) * g   per head (skipped where its norm is
+ *       NULL: q_norm [head_dim] for every query head, k_norm for every key head),
+ *   then the rotation above; values from rot_dim on are not rotated.
+ * q [R][n_heads][head_dim] and k [R][n_kv_heads][head_dim], rows ldq and ldk
+ * apart; q_out, k_out likewise.  An output may be its own input (in place, with
+ * the same stride); otherwise inputs and outputs must not overlap.
+ * pos [n_axes][ldpos] int32, row r's position on axis a at a ldpos + r.
+ * dt: MAP_F32 or MAP_BF16 for q, k, the norms and the outputs; sums and the
+ * rotation are float32, angles float64.  1 <= heads <= 1024 each; R = 0 does
+ * nothing. */
+map_status map_qk_norm_rope(const map_rope* rp, map_dtype dt, int R, int n_heads, int n_kv_heads,
+                            const void* q, int64_t ldq, const void* k, int64_t ldk,
+                            const int32_t* pos, int64_t ldpos, const void* q_norm, const void* k_norm,
+                            void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out, void* stream);
+
+/* A pool of n_pages pages of `page` tokens (16, 32, 64 or 128) for the key and
+ * value heads of one layer, n_kv_heads (at most 256) of head_dim (64 or 128):
+ *   MAP_CACHE_BF16   k, v [n_pages][n_kv_heads][page][head_dim] bf16
+ *   MAP_CACHE_MXFP4  k, v [n_pages][n_kv_heads][page][head_dim / 2] bytes, two
+ *       4-bit codes each (the even value in the low bits: sign, then the level
+ *       0, 0.5, 1, 1.5, 2, 3, 4 or 6), and k_scale, v_scale
+ *       [n_pages][n_kv_heads][page][head_dim / 32] bytes s, one for 32 values:
+ *       a value is its level times 2^(s - 127), or NaN where s is 255.
+ * A sequence's table names its pages in order: token j of sequence b is at
+ * place j % page of page table[b][j / page].  Sequences may share pages that
+ * none of them appends to.  Pointers are 16-byte aligned. */
+typedef enum { MAP_CACHE_BF16 = 0, MAP_CACHE_MXFP4 = 1 } map_cache_type;
+typedef struct {
+  void *k, *v, *k_scale, *v_scale;
+  int32_t type, n_pages, page, n_kv_heads, head_dim;
+} map_cache;
+
+/* The arguments the three calls share:
+ * table [B][max_pages] int32 (device)  page numbers; an entry that is not a
+ *     page of the pool holds nothing: what is appended there is dropped, what is
+ *     read there is zero, and no row sees it (the pages a sliding window has
+ *     left behind may be given back and their entries set to -1)
+ * len   [B] int32 (device)  each sequence's tokens, this call's rows included:
+ *     the sequence's row i of n is its token len[b] - n + i.  Values outside
+ *     0 .. max_pages * page count as the nearest of the two; rows of tokens
+ *     before the sequence's first are dropped, and see nothing.
+ * Both are read on the device when the call runs, so a captured graph can be
+ * replayed while they change. */
+
+/* map_cache_append -- k and v rows [n_kv_heads][head_dim] (rows ldk, ldv apart,
+ * bf16: MAP_ERR_UNSUPPORTED for another dt) to their places.  MAP_CACHE_BF16
+ * keeps them as they are.  MAP_CACHE_MXFP4 takes for each 32 values the smallest
+ * 2^e with max |x| <= 7 * 2^e (-126 <= e <= 125) and each value's nearest level
+ * (ties to the even code; at most 6), so that no value is off by more than half a
+ * step of the levels (but for magnitudes past 7 * 2^125, which become 6 * 2^125);
+ * 32 values that hold an infinity or a NaN become NaN.  Storing what
+ * map_cache_read returned stores the same bytes.  Two rows of one call must
+ * not have the same place (sequences that share the page they append to). */
+map_status map_cache_append(const map_cache* c, map_dtype dt, int B, const int32_t* table, int max_pages,
+                            const int32_t* len, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                            const int32_t* seq_off_host, void* stream);
+
+/* map_cache_read -- cached rows in bf16: row r of sequence b's is its token
+ * slots[r] (device, one for each row of all sequences), or, where slots is NULL,
+ * token r - seq_off[b].  k_out and v_out rows [n_kv_heads][head_dim], ldk and ldv
+ * apart.  A token that the cache does not hold (outside 0 .. len[b] - 1, or no
+ * page) gives zeros.  With the indices of kept tokens as slots, and
+ * map_cache_append of the rows to other pages, it compacts a cache to them. */
+map_status map_cache_read(const map_cache* c, map_dtype dt, int B, const int32_t* table, int max_pages,
+                          const int32_t* len, const int32_t* slots, const int32_t* seq_off_host,
+                          void* k_out, int64_t ldk, void* v_out, int64_t ldv, void* stream);
+
+/* map_cache_attention -- each new row's attention over its sequence's cache
+ * (its own token appended before):
+ *   out[r][h] = softmax(scale q[r][h] K^T) V  over the tokens the row sees, of
+ *   key/value head h / (n_heads / n_kv_heads);
+ * token i sees the tokens j <= i with i - j < window or j < sinks (window = 0:
+ * all of them).  A row that sees nothing gives zeros, and what a row does not
+ * see adds nothing to it, whatever it holds (NaN, infinities).  A score below
+ * -3e38 weighs nothing.
+ * q [rows][n_heads][head_dim] bf16, rows ldq apart; out likewise, ldo apart;
+ * n_heads a multiple of n_kv_heads, at most 1024; 0 < scale < 1e30.  Scores, the softmax and its
+ * sums are float32; probabilities enter the second product as bf16, and so do
+ * the 4-bit values (exactly).  out must not overlap q.
+ * ws: map_cache_attention_workspace() bytes for the same arguments. */
+size_t map_cache_attention_workspace(const map_cache* c, int B, int n_heads, int max_pages,
+                                     const int32_t* seq_off_host);
+map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_heads, const int32_t* table,
+                               int max_pages, const int32_t* len, const void* q, int64_t ldq,
+                               const int32_t* seq_off_host, float scale, int window, int sinks,
+                               void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
 /* map_prune's candidate subset.  A greedy pick of Eq. (4) scores
  * p_i n_i r_i <= p_i n_i, so map_prune may run the selection on a subset J
  * of each image's tokens: R0 plus the tokens with the largest bounds
@@ -376,7 +501,8 @@ map_status map_selection_status(const void* ws, int32_t* status_out, void* strea
  * (enable != 0), map_score, map_similarity, map_select, map_prune,
  * map_prune_assemble, map_prune_noalloc, map_teacher, map_train_step and
  * map_decoder_layer first scan their floating-point inputs (activations,
- * weights, scores, similarities, attention, teacher distributions) on
+ * weights, scores, similarities, attention, teacher distributions; the cache
+ * calls, whose inputs may hold anything in what no row sees, do not) on
  * `stream` for infinities and NaNs, wait for the scan (the call then blocks
  * until the stream has passed it, so it cannot be captured in a graph) and
  * return MAP_ERR_NONFINITE, having enqueued nothing else, if it finds one.

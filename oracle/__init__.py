@@ -23,7 +23,10 @@ Attention in MLLMs for Visual Token Pruning"):
 * ``train``      -- one predictor training step: the KL divergence from the
                     teacher distribution to p_hat and its gradient with
                     respect to every predictor parameter (section
-                    "Cross-Modal Attention Distillation").
+                    "Cross-Modal Attention Distillation");
+* ``cache``      -- the key/value cache of a pruned sequence's later tokens:
+                    head norms and rotation by several position axes, the
+                    4-bit block format, pages, attention over them.
 
 Only the test suite, the smoke entry point and the benchmark's CPU-baseline
 leg may import this package.  The HIP product path never calls it, and it

@@ -24,6 +24,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmap.so")
 MAP_PRUNE_NOALLOC_MAX_BYTES = 96 << 20
 MAP_F32, MAP_BF16 = 0, 1
 MAP_MAX_BATCH, MAP_MAX_N, MAP_MAX_K = 64, 16384, 1024
+MAP_CACHE_BF16, MAP_CACHE_MXFP4 = 0, 1
+MAP_CACHE_MAX_BATCH, MAP_CACHE_MAX_ROWS = 256, 1 << 20
 
 # Every symbol include/map.h declares.
 EXPORTS = (
@@ -31,6 +33,7 @@ EXPORTS = (
     "map_select_workspace", "map_prune_workspace", "map_workspace_bytes", "map_score", "map_similarity", "map_select",
     "map_prune", "map_prune_assemble", "map_prune_noalloc", "map_assemble", "map_teacher_workspace", "map_teacher", "map_set_subset_tokens",
     "map_train_workspace", "map_train_step", "map_decoder_workspace", "map_decoder_layer",
+    "map_qk_norm_rope", "map_cache_append", "map_cache_read", "map_cache_attention_workspace", "map_cache_attention",
     "map_selection_status", "map_set_select_images_per_launch", "map_set_finite_check", "map_timing_enable",
     "map_timing_read",
     "map_timing_reset",
@@ -59,7 +62,19 @@ class map_select_params(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("K0", ctypes.c_int32), ("tau", ctypes.c_float)]
 
 
-_P, _I, _SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+class map_rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("sections", ctypes.c_int32 * 4), ("theta", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
+class map_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("type", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+_P, _I, _SZ, _L, _F = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
 _SIGS = {
     "map_status_string": (ctypes.c_char_p, [_I]),
     "map_version": (_I, []),
@@ -85,6 +100,12 @@ _SIGS = {
                             ctypes.POINTER(map_grads), _P, _SZ, _P]),
     "map_decoder_workspace": (_SZ, [_I, ctypes.POINTER(map_decoder_weights)]),
     "map_decoder_layer": (_I, [ctypes.POINTER(map_decoder_weights), _I, _I, _P, _P, _P, _P, _P, _SZ, _P]),
+    "map_qk_norm_rope": (_I, [ctypes.POINTER(map_rope), _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _P, _L, _P, _L, _P]),
+    "map_cache_append": (_I, [ctypes.POINTER(map_cache), _I, _I, _P, _I, _P, _P, _L, _P, _L, _P, _P]),
+    "map_cache_read": (_I, [ctypes.POINTER(map_cache), _I, _I, _P, _I, _P, _P, _P, _P, _L, _P, _L, _P]),
+    "map_cache_attention_workspace": (_SZ, [ctypes.POINTER(map_cache), _I, _I, _I, _P]),
+    "map_cache_attention": (_I, [ctypes.POINTER(map_cache), _I, _I, _I, _P, _I, _P, _P, _L, _P, _F, _I, _I, _P, _L, _P,
+                                 _SZ, _P]),
     "map_set_subset_tokens": (_I, [_I]),
     "map_selection_status": (_I, [_P, _P, _P]),
     "map_set_select_images_per_launch": (_I, [_I]),
@@ -601,6 +622,263 @@ def decoder_workspace(w: DecoderWeights, R: int, device) -> torch.Tensor:
     if nbytes == 0:
         raise MapError(MAP_ERR_INVALID_ARG, "map_decoder_workspace")
     return _workspace(nbytes, device)
+
+
+class RopeParams:
+    """Rotation by positions of one to four axes: of head_dim values a head, the
+    first rot_dim (None: all) in pairs (i, i + rot_dim / 2); sections gives each
+    axis its number of pairs (None: one axis turns all), in runs or, interleaved,
+    one pair each in turn.  eps is the head norms'."""
+
+    def __init__(self, head_dim: int, rot_dim: Optional[int] = None, sections: Optional[Sequence[int]] = None,
+                 interleaved: bool = False, theta: float = 10000.0, eps: float = 1e-6):
+        rot = head_dim if rot_dim is None else rot_dim
+        sec = [rot // 2] if sections is None else [int(x) for x in sections]
+        if not 1 <= len(sec) <= 4 or sum(sec) != rot // 2 or min(sec) < 0:
+            raise ValueError(f"sections {sec}: one to four pair counts that add up to rot_dim / 2 = {rot // 2}")
+        self.head_dim, self.rot_dim, self.sections = head_dim, rot, sec
+        self._struct = map_rope(head_dim, rot, len(sec), 1 if interleaved else 0,
+                                (ctypes.c_int32 * 4)(*(sec + [0] * (4 - len(sec)))), theta, eps)
+        self._ref = ctypes.byref(self._struct)
+
+
+class SeqOffsets:
+    """Row offsets of a batch of sequences ([B + 1], from 0, not decreasing),
+    checked once; the cache calls take one in place of a list."""
+
+    def __init__(self, seq_off: Sequence[int]):
+        vals = [int(x) for x in (seq_off.tolist() if hasattr(seq_off, "tolist") else seq_off)]
+        if not 2 <= len(vals) <= MAP_CACHE_MAX_BATCH + 1 or vals[0] != 0 or any(b < a for a, b in zip(vals, vals[1:])):
+            raise ValueError(f"offsets: 2 to {MAP_CACHE_MAX_BATCH + 1} entries that start at 0 and do not decrease")
+        if vals[-1] > MAP_CACHE_MAX_ROWS:
+            raise ValueError(f"offsets end at {vals[-1]}: at most {MAP_CACHE_MAX_ROWS} rows a call")
+        self.B, self.rows = len(vals) - 1, vals[-1]
+        self._arr = (ctypes.c_int32 * len(vals))(*vals)
+
+
+class KVCache:
+    """A pool of pages for the keys and values of one layer (include/map.h,
+    map_cache): kind "bf16", or "mxfp4" (4 bits a value, a power of two for each
+    32).  The tensors k, v (and k_scale, v_scale) are the caller's to copy or save;
+    which pages are a sequence's is in the table that each call is given."""
+
+    def __init__(self, n_pages: int, page: int, n_kv_heads: int, head_dim: int, kind: str = "bf16", device="cuda"):
+        if kind not in ("bf16", "mxfp4"):
+            raise ValueError(f"kind {kind!r}: \"bf16\" or \"mxfp4\"")
+        shape = (n_pages, n_kv_heads, page)
+        if kind == "bf16":
+            self._set(*(torch.zeros(shape + (head_dim,), dtype=torch.bfloat16, device=device) for _ in range(2)), None, None)
+        else:
+            self._set(*(torch.zeros(shape + (w,), dtype=torch.uint8, device=device)
+                        for w in (head_dim // 2, head_dim // 2, head_dim // 32, head_dim // 32)))
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                     v_scale: Optional[torch.Tensor] = None) -> "KVCache":
+        """A pool over tensors that exist: bf16 k, v [n_pages, heads, page, head_dim],
+        or uint8 k, v [..., head_dim / 2] with k_scale, v_scale [..., head_dim / 32]."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_scale, v_scale)
+        return self
+
+    def _set(self, k, v, k_scale, v_scale):
+        n_pages, heads, page, width = _dims(k, "k", 4)
+        mx = k_scale is not None
+        dh = 2 * width if mx else width
+        if page not in (16, 32, 64, 128) or dh not in (64, 128) or not 1 <= heads <= 256 or n_pages < 1:
+            raise ValueError(f"a cache has at least one page, of 16, 32, 64 or 128 tokens, 1 to 256 heads and a head_dim "
+                             f"of 64 or 128; got {n_pages}, {page}, {heads} and {dh}")
+        dtype = torch.uint8 if mx else torch.bfloat16
+        for name, t, w, dt in (("k", k, width, dtype), ("v", v, width, dtype)) + (
+                (("k_scale", k_scale, dh // 32, torch.uint8), ("v_scale", v_scale, dh // 32, torch.uint8)) if mx else ()):
+            _need(t, name, (n_pages, heads, page, w), dt, k.device)
+            if t.data_ptr() % 16:
+                raise ValueError(f"{name}: not on a 16-byte boundary")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale if mx else None
+        self.kind, self.device = "mxfp4" if mx else "bf16", k.device
+        self.n_pages, self.page, self.n_kv_heads, self.head_dim = n_pages, page, heads, dh
+        self._struct = map_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if mx else None,
+                                 v_scale.data_ptr() if mx else None, MAP_CACHE_MXFP4 if mx else MAP_CACHE_BF16, n_pages,
+                                 page, heads, dh)
+        self._ref = ctypes.byref(self._struct)
+
+
+def _seq(seq_off) -> SeqOffsets:
+    return seq_off if isinstance(seq_off, SeqOffsets) else SeqOffsets(seq_off)
+
+
+def _rows_ld(t, name: str, rows: int, heads: int, dh: int, dtype, device) -> int:
+    """The row stride of t [>= rows, heads, dh]: heads contiguous in a row, rows
+    any multiple of 16 bytes apart, on a 16-byte boundary."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != dh:
+        raise ValueError(f"{name}: expected {dtype} [at least {rows}, {heads}, {dh}], got {t.dtype} {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+    row, head, one = t.stride()
+    if t.shape[0] <= 1:
+        row = heads * dh
+    if one != 1 or (heads > 1 and head != dh) or row < heads * dh or (row * t.element_size()) % 16 or t.data_ptr() % 16:
+        raise ValueError(f"{name}: heads must be contiguous in a row, rows a multiple of 16 bytes apart and the first on a "
+                         f"16-byte boundary; got strides {t.stride()}")
+    return row
+
+
+def _table(cache: KVCache, table, lens, B: int):
+    """max_pages of a batch's page table [B, max_pages] with lens [B]."""
+    if not isinstance(cache, KVCache):
+        raise TypeError("cache must be a KVCache")
+    _, wide = _dims(table, "table", 2)
+    _need(table, "table", (B, wide), torch.int32, cache.device)
+    _need(lens, "lens", (B,), torch.int32, cache.device)
+    if wide < 1 or wide * cache.page > 1 << 30:
+        raise ValueError(f"table: {wide} pages a sequence")
+    return wide
+
+
+class _on:
+    """The device of a call's tensors as the current one while the library
+    launches on it (nothing to do when it is already)."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return _stream(self.device)
+
+    def __exit__(self, *exc):
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.before)
+
+
+def map_qk_norm_rope(rope: RopeParams, q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor,
+                     q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Head norms (where a norm's weight [head_dim] is given) and rotation of q
+    [R, heads, head_dim] and k [R, kv heads, head_dim] by pos [axes, R] (or [R]
+    for one axis), in one pass.  q and k may be views into a wider row (a qkv
+    product); q_out and k_out may be q and k themselves.  Returns (q_out, k_out)."""
+    R, Hq, dh = _dims(q, "q", 3)
+    _, Hk, _ = _dims(k, "k", 3)
+    dt, dev = _dtype_code(q), q.device
+    if dh != rope.head_dim:
+        raise ValueError(f"q: heads of {dh}, the rotation is for {rope.head_dim}")
+    axes = len(rope.sections)
+    if isinstance(pos, torch.Tensor) and pos.dim() == 1 and axes == 1:
+        pos = pos[None]
+    if not isinstance(pos, torch.Tensor) or pos.dtype != torch.int32 or tuple(pos.shape) != (axes, R) or pos.device != dev \
+            or (R > 1 and pos.stride(1) != 1) or (axes > 1 and pos.stride(0) < R):
+        raise ValueError(f"pos: expected int32 [{axes}, {R}] on {dev}, its rows contiguous")
+    ldq = _rows_ld(q, "q", R, Hq, dh, q.dtype, dev)
+    ldk = _rows_ld(k, "k", R, Hk, dh, q.dtype, dev)
+    for name, g in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if g is not None:
+            _need(g, name, (dh,), q.dtype, dev)
+            if g.data_ptr() % 16:
+                raise ValueError(f"{name}: not on a 16-byte boundary")
+    if q_out is None:
+        q_out = torch.empty(R, Hq, dh, dtype=q.dtype, device=dev)
+    if k_out is None:
+        k_out = torch.empty(R, Hk, dh, dtype=q.dtype, device=dev)
+    ldqo = _rows_ld(q_out, "q_out", R, Hq, dh, q.dtype, dev)
+    ldko = _rows_ld(k_out, "k_out", R, Hk, dh, q.dtype, dev)
+    _on_gpu(q, "q")
+    if R == 0:
+        return q_out, k_out
+    with _on(dev) as stream:
+        _check(lib().map_qk_norm_rope(rope._ref, dt, R, Hq, Hk, q.data_ptr(), ldq, k.data_ptr(), ldk, pos.data_ptr(),
+                                      max(R, pos.stride(0) if axes > 1 else R), None if q_norm is None else q_norm.data_ptr(),
+                                      None if k_norm is None else k_norm.data_ptr(), q_out.data_ptr(), ldqo,
+                                      k_out.data_ptr(), ldko, stream), "map_qk_norm_rope")
+    return q_out, k_out
+
+
+def map_cache_append(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_off):
+    """Stores the new rows k, v [rows, kv heads, head_dim] (bf16; views into a
+    wider row serve): sequence b's are rows seq_off[b] .. seq_off[b+1]-1 and become
+    its last tokens, lens[b] counting them already.  table [B, max_pages] int32
+    names each sequence's pages."""
+    off = _seq(seq_off)
+    wide = _table(cache, table, lens, off.B)
+    ldk = _rows_ld(k, "k", off.rows, cache.n_kv_heads, cache.head_dim, torch.bfloat16, cache.device)
+    ldv = _rows_ld(v, "v", off.rows, cache.n_kv_heads, cache.head_dim, torch.bfloat16, cache.device)
+    _on_gpu(k, "k")
+    if off.rows == 0:
+        return
+    with _on(cache.device) as stream:
+        _check(lib().map_cache_append(cache._ref, MAP_BF16, off.B, table.data_ptr(), wide, lens.data_ptr(), k.data_ptr(), ldk,
+                                      v.data_ptr(), ldv, off._arr, stream), "map_cache_append")
+
+
+def map_cache_read(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, seq_off, slots: Optional[torch.Tensor] = None,
+                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """Cached keys and values in bf16, [rows, kv heads, head_dim] each: row r of
+    sequence b's is its token slots[r] (int32), or token r - seq_off[b].  Tokens
+    that the cache does not hold give zeros.  Returns (k_out, v_out)."""
+    off = _seq(seq_off)
+    wide = _table(cache, table, lens, off.B)
+    shape = (off.rows, cache.n_kv_heads, cache.head_dim)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    ldk = _rows_ld(k_out, "k_out", *shape, torch.bfloat16, cache.device)
+    ldv = _rows_ld(v_out, "v_out", *shape, torch.bfloat16, cache.device)
+    if slots is not None:
+        _need(slots, "slots", (off.rows,), torch.int32, cache.device)
+    _on_gpu(k_out, "k_out")
+    if off.rows == 0:
+        return k_out, v_out
+    with _on(cache.device) as stream:
+        _check(lib().map_cache_read(cache._ref, MAP_BF16, off.B, table.data_ptr(), wide, lens.data_ptr(),
+                                    None if slots is None else slots.data_ptr(), off._arr, k_out.data_ptr(), ldk,
+                                    v_out.data_ptr(), ldv, stream), "map_cache_read")
+    return k_out, v_out
+
+
+def cache_attention_workspace(cache: KVCache, seq_off, n_heads: int, table: torch.Tensor) -> torch.Tensor:
+    """A reusable workspace for map_cache_attention over these rows, heads and table."""
+    off = _seq(seq_off)
+    nbytes = lib().map_cache_attention_workspace(cache._ref, off.B, n_heads, _dims(table, "table", 2)[1], off._arr)
+    if nbytes == 0:
+        raise MapError(MAP_ERR_INVALID_ARG, "map_cache_attention_workspace")
+    return _workspace(nbytes, cache.device)
+
+
+def map_cache_attention(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, seq_off,
+                        scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+                        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Attention of the new rows q [rows, heads, head_dim] (bf16) over their
+    sequences' cached tokens, their own (appended before) included: token i sees
+    the tokens j <= i with i - j < window (0: no window) or j < sinks.  scale is
+    1 / sqrt(head_dim) by default.  Returns out, shaped like q; rows from
+    seq_off[B] on are not touched."""
+    off = _seq(seq_off)
+    wide = _table(cache, table, lens, off.B)
+    rows, heads, dh = _dims(q, "q", 3)
+    ldq = _rows_ld(q, "q", off.rows, heads, cache.head_dim, torch.bfloat16, cache.device)
+    if out is None:
+        out = torch.empty(rows, heads, dh, dtype=torch.bfloat16, device=cache.device)
+    ldo = _rows_ld(out, "out", off.rows, heads, dh, torch.bfloat16, cache.device)
+    if heads % cache.n_kv_heads or not 1 <= heads <= 1024:
+        raise ValueError(f"q: {heads} heads over {cache.n_kv_heads} key/value heads")
+    if window < 0 or sinks < 0:
+        raise ValueError("window and sinks must not be negative")
+    _on_gpu(q, "q")
+    if off.rows == 0:
+        return out
+    ws = cache_attention_workspace(cache, off, heads, table) if workspace is None else workspace
+    _need_ws(ws, 256, cache.device)
+    with _on(cache.device) as stream:
+        _check(lib().map_cache_attention(cache._ref, MAP_BF16, off.B, heads, table.data_ptr(), wide, lens.data_ptr(),
+                                         q.data_ptr(), ldq, off._arr, dh ** -0.5 if scale is None else float(scale),
+                                         int(window), int(sinks), out.data_ptr(), ldo, ws.data_ptr(), ws.numel(), stream),
+               "map_cache_attention")
+    return out
 
 
 def selection_status(ws: torch.Tensor) -> int:

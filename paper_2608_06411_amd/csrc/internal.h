@@ -430,6 +430,54 @@ hipError_t launch_silu_mul(const DecoderArgs& a, hipStream_t s);
 // 1) + res, both [M][ldc] bf16
 hipError_t launch_splitk_resid(const GemmProblem& P, const void* res, void* out, int ldc, hipStream_t s);
 
+// ---------------------------------------------------------------- key/value cache
+// Head rotation (map_qk_norm_rope).
+struct QkRopeArgs {
+  const void *q, *k;
+  void *q_out, *k_out;
+  long long ldq, ldk, ldqo, ldko;  // in elements
+  const int32_t* pos;              // axis a of row r at a ldpos + r
+  long long ldpos;
+  const void *q_norm, *k_norm;     // [head_dim] or null
+  int R, Hq, Hkv, Dh, rot, parts;  // parts: waves that share a row's heads
+  float eps;
+  uint8_t axis[64];                // position axis of each pair
+  double turns[64];                // theta^(-2i/rot) / (2 pi): turns of pair i per position
+};
+hipError_t launch_qk_norm_rope(map_dtype dt, QkRopeArgs& a, hipStream_t s);
+
+// The pages, as the kernels see them.
+struct CachePages {
+  void *k, *v;
+  uint8_t *ks, *vs;       // scale bytes (MXFP4)
+  const int32_t* table;   // [B][max_pages]
+  const int32_t* len;     // [B]
+  int n_pages, shift, heads, max_pages;  // page = 1 << shift
+};
+struct CacheRowsArgs {
+  CachePages c;
+  void *k, *v;            // rows: read by append, written by read
+  long long ldk, ldv;
+  const int32_t* slots;   // read only: each row's token (null: its place in the sequence)
+  int B, Dh, parts;       // parts: workgroups that share a tile's heads
+  bool fp4;
+  int off[MAP_CACHE_MAX_BATCH + 1];
+};
+hipError_t launch_cache_append(CacheRowsArgs& a, hipStream_t s);
+hipError_t launch_cache_read(CacheRowsArgs& a, hipStream_t s);
+
+struct CacheAttnArgs {
+  CachePages c;
+  const void* q;
+  void* out;
+  long long ldq, ldo;
+  int B, Hq, G, Dh, window, sinks;
+  float c2;               // scale log2(e)
+  bool fp4;
+  int off[MAP_CACHE_MAX_BATCH + 1];
+};
+hipError_t launch_cache_attention(CacheAttnArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- teacher selection
 constexpr int kTeacherMaxLayers = 256;
 constexpr int kTeacherMaxSlices = 16;

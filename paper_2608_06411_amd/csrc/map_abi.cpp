@@ -1479,6 +1479,202 @@ map_status map_decoder_layer(const map_decoder_weights* w, map_dtype dt, int B, 
   return hip_status(enqueue_decoder(*w, B, X, pos, seq_off_host, Y, t, cus, static_cast<hipStream_t>(stream)));
 }
 
+// ------------------------------------------------------------ key/value cache
+extern "C++" {
+namespace {
+
+bool aligned16(std::initializer_list<const void*> ptrs) {
+  uintptr_t any = 0;
+  for (const void* p : ptrs) any |= reinterpret_cast<uintptr_t>(p);
+  return (any & 15) == 0;
+}
+
+// A row stride: at least the row, and a whole number of 16-byte pieces.
+bool valid_ld(int64_t ld, int64_t row, size_t elem) {
+  return ld >= row && ld <= (int64_t)1 << 32 && ld * static_cast<int64_t>(elem) % 16 == 0;
+}
+
+bool valid_rope(const map_rope* rp) {
+  if (!rp || (rp->head_dim != 64 && rp->head_dim != 128) || rp->rot_dim < 16 || rp->rot_dim > rp->head_dim ||
+      rp->rot_dim % 16 != 0 || rp->n_axes < 1 || rp->n_axes > 4 || !isfinite(rp->theta) || rp->theta <= 0.0f ||
+      !isfinite(rp->eps) || rp->eps < 0.0f)
+    return false;
+  long long pairs = 0;
+  for (int a = 0; a < rp->n_axes; ++a) {
+    if (rp->sections[a] < 0 || rp->sections[a] > rp->rot_dim / 2) return false;
+    pairs += rp->sections[a];
+  }
+  return pairs == rp->rot_dim / 2;
+}
+
+// The axis of each pair: runs, or one pair each in turn while they have some.
+void rope_axes(const map_rope& rp, uint8_t* axis) {
+  int left[4] = {rp.sections[0], rp.sections[1], rp.sections[2], rp.sections[3]}, a = 0;
+  for (int i = 0; i < rp.rot_dim / 2; ++i) {
+    while (left[a] == 0) a = (a + 1) % rp.n_axes;
+    axis[i] = static_cast<uint8_t>(a);
+    --left[a];
+    if (rp.interleaved) a = (a + 1) % rp.n_axes;
+  }
+}
+
+bool valid_cache(const map_cache* c) {
+  return c && c->k && c->v && (c->type == MAP_CACHE_BF16 || c->type == MAP_CACHE_MXFP4) && c->n_pages >= 1 &&
+         (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) && c->n_kv_heads >= 1 &&
+         c->n_kv_heads <= 256 && (c->head_dim == 64 || c->head_dim == 128) &&
+         (c->type == MAP_CACHE_BF16 || (c->k_scale && c->v_scale)) && aligned16({c->k, c->v, c->k_scale, c->v_scale});
+}
+
+// max_pages * page, the most tokens a sequence can have, stays an int.
+bool valid_table(const map_cache& c, int max_pages) {
+  return max_pages >= 1 && (long long)max_pages * c.page <= (1 << 30);
+}
+
+bool valid_rows(const int32_t* off, int B) {
+  if (B < 1 || B > MAP_CACHE_MAX_BATCH || !off || off[0] != 0) return false;
+  for (int b = 0; b < B; ++b)
+    if (off[b + 1] < off[b]) return false;
+  return off[B] <= MAP_CACHE_MAX_ROWS;
+}
+
+CachePages cache_pages(const map_cache& c, const int32_t* table, int max_pages, const int32_t* len) {
+  CachePages p;
+  p.k = c.k;
+  p.v = c.v;
+  p.ks = static_cast<uint8_t*>(c.k_scale);
+  p.vs = static_cast<uint8_t*>(c.v_scale);
+  p.table = table;
+  p.len = len;
+  p.n_pages = c.n_pages;
+  p.shift = c.page == 16 ? 4 : c.page == 32 ? 5 : c.page == 64 ? 6 : 7;
+  p.heads = c.n_kv_heads;
+  p.max_pages = max_pages;
+  return p;
+}
+
+map_status cache_rows_args(CacheRowsArgs& a, const map_cache* c, map_dtype dt, int B, const int32_t* table,
+                           int max_pages, const int32_t* len, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           const int32_t* off) {
+  if (!valid_dtype(dt) || !valid_cache(c) || !table || !len || !valid_table(*c, max_pages) || !k || !v ||
+      !valid_rows(off, B) || !aligned16({k, v}))
+    return MAP_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)c->n_kv_heads * c->head_dim;
+  if (!valid_ld(ldk, row, 2) || !valid_ld(ldv, row, 2)) return MAP_ERR_INVALID_ARG;
+  if (dt != MAP_BF16) return MAP_ERR_UNSUPPORTED;
+  a.c = cache_pages(*c, table, max_pages, len);
+  a.k = const_cast<void*>(k);
+  a.v = const_cast<void*>(v);
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.slots = nullptr;
+  a.B = B;
+  a.Dh = c->head_dim;
+  a.fp4 = c->type == MAP_CACHE_MXFP4;
+  std::copy(off, off + B + 1, a.off);
+  return MAP_OK;
+}
+
+}  // namespace
+}  // extern "C++"
+
+map_status map_qk_norm_rope(const map_rope* rp, map_dtype dt, int R, int n_heads, int n_kv_heads, const void* q,
+                            int64_t ldq, const void* k, int64_t ldk, const int32_t* pos, int64_t ldpos,
+                            const void* q_norm, const void* k_norm, void* q_out, int64_t ldq_out, void* k_out,
+                            int64_t ldk_out, void* stream) {
+  if (!valid_dtype(dt) || !valid_rope(rp) || R < 0 || R > MAP_CACHE_MAX_ROWS || n_heads < 1 || n_heads > 1024 ||
+      n_kv_heads < 1 || n_kv_heads > 1024 || !q || !k || !pos || !q_out || !k_out ||
+      !aligned16({q, k, q_norm, k_norm, q_out, k_out}))
+    return MAP_ERR_INVALID_ARG;
+  const int64_t rq = (int64_t)n_heads * rp->head_dim, rk = (int64_t)n_kv_heads * rp->head_dim;
+  const size_t es = elem_size(dt);
+  if (!valid_ld(ldq, rq, es) || !valid_ld(ldk, rk, es) || !valid_ld(ldq_out, rq, es) || !valid_ld(ldk_out, rk, es) ||
+      ldpos < R || ldpos > (int64_t)1 << 32 || (q == q_out && ldq != ldq_out) || (k == k_out && ldk != ldk_out))
+    return MAP_ERR_INVALID_ARG;
+  if (R == 0) return MAP_OK;
+  QkRopeArgs a;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldqo = ldq_out;
+  a.ldko = ldk_out;
+  a.pos = pos;
+  a.ldpos = ldpos;
+  a.q_norm = q_norm;
+  a.k_norm = k_norm;
+  a.R = R;
+  a.Hq = n_heads;
+  a.Hkv = n_kv_heads;
+  a.Dh = rp->head_dim;
+  a.rot = rp->rot_dim;
+  a.eps = rp->eps;
+  rope_axes(*rp, a.axis);
+  for (int i = 0; i < rp->rot_dim / 2; ++i)
+    a.turns[i] = pow(static_cast<double>(rp->theta), -2.0 * i / rp->rot_dim) / (2.0 * M_PI);
+  return hip_status(launch_qk_norm_rope(dt, a, static_cast<hipStream_t>(stream)));
+}
+
+map_status map_cache_append(const map_cache* c, map_dtype dt, int B, const int32_t* table, int max_pages,
+                            const int32_t* len, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                            const int32_t* seq_off_host, void* stream) {
+  CacheRowsArgs a;
+  const map_status ok = cache_rows_args(a, c, dt, B, table, max_pages, len, k, ldk, v, ldv, seq_off_host);
+  if (ok != MAP_OK || a.off[B] == 0) return ok;
+  return hip_status(launch_cache_append(a, static_cast<hipStream_t>(stream)));
+}
+
+map_status map_cache_read(const map_cache* c, map_dtype dt, int B, const int32_t* table, int max_pages,
+                          const int32_t* len, const int32_t* slots, const int32_t* seq_off_host, void* k_out,
+                          int64_t ldk, void* v_out, int64_t ldv, void* stream) {
+  CacheRowsArgs a;
+  const map_status ok = cache_rows_args(a, c, dt, B, table, max_pages, len, k_out, ldk, v_out, ldv, seq_off_host);
+  if (ok != MAP_OK || a.off[B] == 0) return ok;
+  a.slots = slots;
+  return hip_status(launch_cache_read(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t map_cache_attention_workspace(const map_cache* c, int B, int n_heads, int max_pages,
+                                     const int32_t* seq_off_host) {
+  if (!valid_cache(c) || !valid_table(*c, max_pages) || !valid_rows(seq_off_host, B) || n_heads < 1 ||
+      n_heads > 1024 || n_heads % c->n_kv_heads != 0)
+    return 0;
+  return kAlign;
+}
+
+map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_heads, const int32_t* table,
+                               int max_pages, const int32_t* len, const void* q, int64_t ldq,
+                               const int32_t* seq_off_host, float scale, int window, int sinks, void* out,
+                               int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
+  const size_t need = map_cache_attention_workspace(c, B, n_heads, max_pages, seq_off_host);
+  if (!valid_dtype(dt) || need == 0 || !table || !len || !q || !out || !aligned16({q, out}) || !(scale > 0.0f && scale < 1e30f) ||
+      window < 0 || sinks < 0)
+    return MAP_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)n_heads * c->head_dim;
+  if (!valid_ld(ldq, row, 2) || !valid_ld(ldo, row, 2)) return MAP_ERR_INVALID_ARG;
+  if (dt != MAP_BF16) return MAP_ERR_UNSUPPORTED;
+  const map_status ws_ok = check_ws(ws, ws_bytes, need);
+  if (ws_ok != MAP_OK) return ws_ok;
+  if (seq_off_host[B] == 0) return MAP_OK;
+  CacheAttnArgs a;
+  a.c = cache_pages(*c, table, max_pages, len);
+  a.q = q;
+  a.out = out;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.B = B;
+  a.Hq = n_heads;
+  a.G = n_heads / c->n_kv_heads;
+  a.Dh = c->head_dim;
+  a.window = window;
+  a.sinks = sinks;
+  a.c2 = static_cast<float>(scale * 1.4426950408889634);
+  a.fp4 = c->type == MAP_CACHE_MXFP4;
+  std::copy(seq_off_host, seq_off_host + B + 1, a.off);
+  return hip_status(launch_cache_attention(a, static_cast<hipStream_t>(stream)));
+}
+
 map_status map_set_finite_check(int enable) {
   g_finite_check.store(enable != 0 ? 1 : 0);
   return MAP_OK;
