@@ -1,112 +1,756 @@
 // Attention of new rows over their sequences' cached keys and values.
 //
 //   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(c2 <q, k_j> - m),  over the tokens
-//   the row sees; c2 = scale log2(e), m the running maximum (one pass).
+//   j the row sees; c2 = scale log2(e), m the running maximum (one pass).
 //
-// A workgroup takes one row and head; its four waves take 64 tokens each in
-// turn, a token a lane for the scores and two values a lane for the sum, and
-// join their (m, l, o) at the end.
+// Both products are formed transposed on the matrix cores, S^T = K Q^T and
+// O^T = V^T P^T, so that a lane holds one query (a column) throughout: the
+// maximum and the sums are over its own registers and an exchange or two, the
+// statistics and the rescaling are per lane, and the scores become the second
+// product's operand in place, its keys taken in the order in which the lane
+// holds them.  V passes through LDS row by row as it lies in the pages, and the
+// transposing LDS reads (ds_read_b64_tr_b16: 16 lanes give the addresses of 4
+// keys' 16 values and get a value's 4 keys each) bring it to that order.
+// 4-bit values are widened to bf16 on their way to the registers (keys) or to
+// LDS (values), scale and all, which is exact.
+//
+// Output rows are rescaled only when a row's maximum has grown by more than
+// 2^6 (the sums carry the same factor, so the result is the same softmax).  m
+// starts below every score that counts but finite, so that a row whose scores so
+// far are all -inf, or all hidden, has zero probabilities there.
+#include <type_traits>
+
 #include "cache_pages.h"
 
 namespace mapk {
 
 namespace {
 
-constexpr int NT = 256;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+
+constexpr float kLow = -3.0e38f;   // m before the first visible score
+constexpr float kRescale = 6.0f;   // log2 of the growth that a row's factor may lag behind
+
+__device__ __forceinline__ s16x4_t tr_read(const void* p) {
+  typedef __attribute__((address_space(3))) s16x4_t lds_t;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_t*)(__attribute__((address_space(3))) void*)const_cast<void*>(p));
+}
+__device__ __forceinline__ bf16x8_t join(s16x4_t a, s16x4_t b) {
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Two bf16 in a word, infinities and NaN cleared.
+__device__ __forceinline__ uint32_t word_clean(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+  return w;
+}
+__device__ __forceinline__ bf16x8_t clean8(bf16x8_t v) {
+  const uint4 u = __builtin_bit_cast(uint4, v);
+  return __builtin_bit_cast(bf16x8_t, make_uint4(word_clean(u.x), word_clean(u.y), word_clean(u.z), word_clean(u.w)));
+}
+
+// The blocks of KB tokens that rows lo .. hi - 1 (token indices) see any of:
+// those of the first tokens, then those from the first row's window to the last row.
+struct Blocks {
+  int sink, first, count;  // blocks 0 .. sink - 1, then from `first`
+  __device__ __forceinline__ int token(int j, int kb) const { return (j < sink ? j : j - sink + first) * kb; }
+};
+__device__ __forceinline__ Blocks visible_blocks(int lo, int hi, int window, int sinks, int kb) {
+  Blocks r;
+  const int end = hi > 0 ? (hi + kb - 1) / kb : 0;
+  const int from = window > 0 ? max(0, lo - window + 1) / kb : 0;
+  r.sink = window > 0 ? min(min(sinks, max(hi, 0)) / kb + (min(sinks, max(hi, 0)) % kb ? 1 : 0), from) : 0;
+  r.first = from;
+  r.count = r.sink + max(0, end - from);
+  return r;
+}
+
+// ---------------------------------------------------------------- few rows
+// Single tokens and a few rows behind a cache.  A workgroup takes 16 columns, the
+// (row, query head) pairs of one key/value head, and one of S parts of the tokens;
+// each of its four waves streams every fourth block of that part on its own (no
+// barrier until the end) and they join.  Bound: the cache's bytes.  A block's
+// keys and values are loaded a block ahead, straight to registers (16 bytes a
+// lane: keys as the first product's operand, values on their way to LDS), so that
+// each wave always has a block in flight; the matrix products and the
+// softmax (a few hundred clocks a block) hide behind them.
+constexpr int kStepWaves = 4;
+
+template <int DH, bool FP4> struct StepShape {
+  static constexpr int KB = 32, NT = KB / 16, NM = KB / 32, ND = DH / 16, NS = DH / 32;
+  static constexpr int VROW = 2 * DH;                       // bytes of a token's values in LDS
+  static constexpr int VPIECE = FP4 ? DH / 2 : 2 * DH;      // and in a page
+  static constexpr int NV = KB * VPIECE / 1024;             // 16-byte pieces a lane
+  static constexpr int OLD = DH + 4;                        // floats between joined rows
+  static constexpr int BYTES = kStepWaves * (KB * VROW > 16 * OLD * 4 ? KB * VROW : 16 * OLD * 4);
+};
+
+// Position of 32-byte chunk c of key k's row in LDS (16 keys' chunks spread over all banks).
+template <int DH> __device__ __forceinline__ int vchunk(int c, int k) {
+  return DH == 128 ? c ^ (k & 7) : c ^ ((k >> 1) & 3);
+}
 
 template <int DH, bool FP4>
-__global__ __launch_bounds__(NT) void cache_attention_kernel(const CacheAttnArgs a) {
-  __shared__ float qs[DH], os[4][DH], ms[4], ls[4];
-  __shared__ float ps[4][64];
-  __shared__ long long rs[4][64];
-  const int b = blockIdx.z, h = blockIdx.y, i = blockIdx.x, r0 = a.off[b], n = a.off[b + 1] - r0;
-  if (i >= n) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, kvh = h / a.G;
-  const int len = cache_len(a.c, b), me = len - n + i;
-  if (threadIdx.x < DH)
-    qs[threadIdx.x] = bf16_to_f32(static_cast<const bf16_t*>(a.q)[(r0 + i) * a.ldq + h * DH + threadIdx.x]);
-  __syncthreads();
-  float m = -3.0e38f, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int j0 = 64 * wave; j0 <= me; j0 += 256) {
-    const int j = j0 + lane;
-    const bool see = j <= me && (a.window == 0 || me - j < a.window || j < a.sinks);
-    const int page = see ? cache_page(a.c, b, j) : -1;
-    const long long row = page >= 0 ? cache_row(a.c, page, kvh, j) : -1;
-    float z = -INFINITY;
-    if (row >= 0) {
-      float sum = 0.0f;
-      for (int d = 0; d < DH; d += 8) {
-        union { uint4 u; bf16_t e[8]; } k;
-        if constexpr (FP4)
-          k.u = fp4_eight(static_cast<const uint32_t*>(a.c.k)[row * (DH / 8) + d / 8], fp4_scale(a.c.ks[row * (DH / 32) + d / 32]));
-        else
-          k.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.k) + row * DH + d);
+__global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const CacheAttnArgs a) {
+  using X = StepShape<DH, FP4>;
+  constexpr int KB = X::KB, NT = X::NT, NM = X::NM, ND = X::ND, NS = X::NS, NV = X::NV;
+  __shared__ __attribute__((aligned(1024))) char lds[X::BYTES];
+  __shared__ float ms[kStepWaves][16], ls[kStepWaves][16];
+  const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
+  const int kvh = blockIdx.y / a.tiles, col0 = (blockIdx.y - kvh * a.tiles) * 16, cols = n * a.G;
+  if (n > a.step_rows || col0 >= cols) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lc = lane & 15, g4 = lane >> 4;
+  const int len = cache_len(a.c, b), base = len - n;  // token of the sequence's first new row
+  const int i_lo = col0 / a.G, i_hi = min(col0 + 15, cols - 1) / a.G;
+  const int lo = base + i_lo, hi = base + i_hi + 1;
+  const Blocks blocks = visible_blocks(lo, hi, a.window, a.sinks, KB);
+  const int part = blockIdx.x, j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.splits);
+  const int j0 = static_cast<int>((long long)blocks.count * part / a.splits) + wave;
+
+  // this lane's query
+  const int col = min(col0 + lc, cols - 1), row = col / a.G, head = kvh * a.G + col - row * a.G, me = base + row;
+  bf16x8_t qf[NS];
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (r0 + row) * a.ldq + head * DH;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(qs[d + e], bf16_to_f32(k.e[e]), sum);
-      }
-      z = sum * a.c2;
+    for (int st = 0; st < NS; ++st)
+      qf[st] = *reinterpret_cast<const bf16x8_t*>(q + (FP4 ? (DH / 4) * g4 + 8 * st : 32 * st + 8 * g4));
+  }
+
+  // A block on its way: keys as they lie in the pages, values, scale bytes.
+  uint4 kr[FP4 ? 1 : NT][FP4 ? 1 : NS], vr[NV];
+  uint32_t kw[FP4 ? NT : 1][NS];
+  uint32_t ksb[NT], vsb[NV];
+  int ent[NT];  // pages of the block's 16-token tiles (-1: none)
+  auto load_pages = [&](int t0) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int tok = t0 + 16 * t;
+      ent[t] = tok < len ? cache_page(a.c, b, tok) : -1;
     }
-    float mx = z;
+  };
+  auto tile_row = [&](int t, int t0) {  // (a tile without a page reads the pool's first tokens, masked)
+    return ent[t] >= 0 ? cache_row(a.c, ent[t], kvh, t0 + 16 * t) : 0LL;
+  };
+  auto load_block = [&](int t0) {
+    long long rows[NT];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-    const float mn = fmaxf(m, mx), al = exp2f(m - mn);
-    m = mn;
-    const float p = row >= 0 ? exp2f(z - m) : 0.0f;
-    l = l * al + p;
-    o0 *= al;
-    o1 *= al;
-    ps[wave][lane] = p;
-    rs[wave][lane] = row;
-    for (int t = 0; t < 64; ++t) {
-      const long long vr = rs[wave][t];
-      if (vr < 0) continue;
-      const float pt = ps[wave][t];
-      if (DH == 64 && lane >= 32) continue;
-      uint32_t w;
+    for (int t = 0; t < NT; ++t) rows[t] = tile_row(t, t0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const long long r = rows[t] + lc;
       if constexpr (FP4) {
-        const uint32_t byte = static_cast<const uint8_t*>(a.c.v)[vr * (DH / 2) + lane];
-        w = fp4_pair<0>(byte, fp4_scale(a.c.vs[vr * (DH / 32) + lane / 16]));
+        const char* p = static_cast<const char*>(a.c.k) + r * (DH / 2) + g4 * (DH / 8);
+        if constexpr (DH == 128) {
+          const uint4 w = *reinterpret_cast<const uint4*>(p);
+          kw[t][0] = w.x;
+          kw[t][1] = w.y;
+          kw[t][NS - 2] = w.z;
+          kw[t][NS - 1] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(p);
+          kw[t][0] = w.x;
+          kw[t][1] = w.y;
+        }
+        ksb[t] = a.c.ks[r * NS + g4 * NS / 4];
       } else {
-        w = reinterpret_cast<const uint32_t*>(static_cast<const bf16_t*>(a.c.v) + vr * DH)[lane];
-      }
-      o0 = fmaf(pt, __uint_as_float(w << 16), o0);
-      o1 = fmaf(pt, __uint_as_float(w & 0xffff0000u), o1);
-    }
-  }
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
-  if (2 * lane < DH) {
-    os[wave][2 * lane] = o0;
-    os[wave][2 * lane + 1] = o1;
-  }
-  if (lane == 0) {
-    ms[wave] = m;
-    ls[wave] = l;
-  }
-  __syncthreads();
-  if (threadIdx.x < DH) {
-    const float mm = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-    float o = 0.0f, sum = 0.0f;
-    for (int w = 0; w < 4; ++w) {
-      const float f = exp2f(ms[w] - mm);
-      o = fmaf(f, os[w][threadIdx.x], o);
-      sum = fmaf(f, ls[w], sum);
+        for (int st = 0; st < NS; ++st)
+          kr[t][st] = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.k) + r * DH + 32 * st + 8 * g4);
+      }
     }
-    static_cast<bf16_t*>(a.out)[(r0 + i) * a.ldo + h * DH + threadIdx.x] = f32_to_bf16(sum == 0.0f ? 0.0f : o / sum);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      constexpr int PPK = X::VPIECE / 16;  // pieces a key
+      const int e = u * 64 + lane, key = e / PPK, c = e % PPK;
+      const long long r = (NT == 1 || key < 16 ? rows[0] : rows[NT - 1]) + (key & 15);
+      vr[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * X::VPIECE + 16 * c);
+      if constexpr (FP4) vsb[u] = a.c.vs[r * NS + c];
+    }
+  };
+
+  f32x4_t o[ND];  // O^T: rows 16 d + 4 g4 + (0..3) = values, column lc = the query
+  float m, l;
+  char* vt = lds + wave * KB * X::VROW;
+  const int tr_key = 4 * g4 + (lc >> 2);  // the key and 8 bytes this lane names for a transposing read
+  const char* tr_at = vt + tr_key * X::VROW + 8 * (lc & 3);
+
+  // The block's tokens that this lane's row sees, and that any row of the tile sees:
+  // from its window on, up to itself, and the first tokens.
+  const int from = a.window > 0 ? me - a.window + 1 : 0, from_lo = a.window > 0 ? lo - a.window + 1 : 0;
+  auto sees = [&](int cur, int k, uint32_t page) {
+    const int tok = cur + k;
+    return static_cast<bool>((page != 0u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
+  };
+  auto run = [&](auto careful) {
+  m = kLow;
+  l = 0.0f;
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  int j = j0, t0 = 0;
+  if (j < j_end) {
+    t0 = blocks.token(j, KB);
+    load_pages(t0);
+    load_block(t0);
   }
+  while (j < j_end) {
+    // what of the block can be seen: all of it by every row, or token by token
+    bool pages = true;
+    uint32_t held = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      pages = pages && ent[t] >= 0;
+      held |= ent[t] >= 0 ? 1u << t : 0u;
+    }
+    const int cur = t0;
+    const bool whole = pages && cur + KB - 1 <= lo && (a.window == 0 || hi - 1 - cur < a.window || cur + KB <= a.sinks);
+    // S^T
+    f32x4_t sc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      sc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        bf16x8_t kf;
+        if constexpr (FP4) kf = __builtin_bit_cast(bf16x8_t, fp4_eight(kw[t][st], fp4_scale(ksb[t])));
+        else kf = __builtin_bit_cast(bf16x8_t, kr[t][st]);
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], sc[t], 0, 0, 0);
+      }
+    }
+    // V to LDS; a token that no row of the tile sees is zeroed (its values may be anything)
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      constexpr int PPK = X::VPIECE / 16;
+      const int e = u * 64 + lane, key = e / PPK, c = e % PPK, tok = cur + key;
+      const bool see = whole | (((held >> (key >> 4)) & 1u) & (tok < hi) & ((tok >= from_lo) | (tok < a.sinks)));
+      if constexpr (FP4) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t w = x == 0 ? vr[u].x : x == 1 ? vr[u].y : x == 2 ? vr[u].z : vr[u].w;
+          uint4 v = fp4_eight(w, fp4_scale(vsb[u]));
+          if (!see) v = make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) = v;
+        }
+      } else {
+        uint4 v = vr[u];
+        if (!see) v = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(c >> 1, key) + 16 * (c & 1)) = v;
+      }
+    }
+    // the next block's loads under the rest of this one
+    j += kStepWaves;
+    if (j < j_end) {
+      t0 = blocks.token(j, KB);
+      load_pages(t0);
+      load_block(t0);
+    }
+    // the row's maximum and probabilities
+    float z[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[t][r] = sc[t][r];
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[t][r] = sees(cur, 16 * t + 4 * g4 + r, (held >> t) & 1u) ? z[t][r] : -INFINITY;
+    }
+    float mx = z[0][0];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, z[t][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.c2;
+    const bool grow = mx > m + kRescale;
+    if (__any(grow)) {
+      const float al = grow ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;  // (first block: 0)
+      if (grow) m = mx;
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= al;
+    }
+    bf16x8_t pf[NM];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(z[t][r], a.c2, -m));
+        l += p;
+        pf[t >> 1][4 * (t & 1) + r] = static_cast<__bf16>(p);
+      }
+    // O^T += V^T P^T
+    auto vfrag = [&](int x, int d) {
+      const char* at = tr_at + 32 * x * X::VROW + 32 * vchunk<DH>(d, tr_key);
+      return join(tr_read(at), tr_read(at + 16 * X::VROW));
+    };
+    if constexpr (careful.value) {
+#pragma unroll
+      for (int x = 0; x < NM; ++x)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(clean8(vfrag(x, d)), pf[x], o[d], 0, 0, 0);
+      for (int k = 0; k < KB; ++k) {
+        const bool see = sees(cur, k, (held >> (k >> 4)) & 1u);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bf16_t v = *reinterpret_cast<const bf16_t*>(vt + k * X::VROW + 32 * vchunk<DH>(d, k) + 2 * (4 * g4 + r));
+            o[d][r] += (see & ((v & 0x7f80) == 0x7f80)) ? bf16_to_f32(v) : 0.0f;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < NM; ++x)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag(x, d), pf[x], o[d], 0, 0, 0);
+    }
+  }
+  };
+  // Every value taken as finite; if a sum comes out infinite or NaN and the tile
+  // has several rows, once more keeping such values from the rows that do not see
+  // them (their zero probability would not cancel them): the product runs on the
+  // finite values, the others add themselves to the rows that see them.
+  run(std::false_type{});
+  if (i_lo != i_hi) {
+    f32x4_t any = {0.0f, 0.0f, 0.0f, 0.0f};  // NaN once a sum is not finite
+#pragma unroll
+    for (int d = 0; d < ND; ++d) any += o[d] * 0.0f;
+    if (__any(any[0] + any[1] + any[2] + any[3] != 0.0f)) run(std::true_type{});
+  }
+
+  // join the waves
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g4 == 0) {
+    ms[wave][lc] = m;
+    ls[wave][lc] = l;
+  }
+  __syncthreads();  // (V is read out)
+  float* os = reinterpret_cast<float*>(lds) + wave * 16 * X::OLD;
+#pragma unroll
+  for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4_t*>(os + lc * X::OLD + 16 * d + 4 * g4) = o[d];
+  __syncthreads();
+  constexpr int PER = DH / 16;  // values a thread
+  const int c = tid >> 4, d0 = (tid & 15) * PER;
+  if (col0 + c >= cols) return;
+  float mm = kLow, sum = 0.0f, v[PER];
+#pragma unroll
+  for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, ms[w][c]);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) v[k] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kStepWaves; ++w) {
+    const float lw = ls[w][c], f = lw == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ms[w][c] - mm);
+    if (lw == 0.0f) continue;
+    sum = fmaf(f, lw, sum);
+    const float* src = reinterpret_cast<const float*>(lds) + (w * 16 + c) * X::OLD + d0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) v[k] = fmaf(f, src[k], v[k]);
+  }
+  const int rr = (col0 + c) / a.G, hh = kvh * a.G + col0 + c - rr * a.G;
+  if (a.splits == 1) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    bf16_t* out = static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0;
+    union { uint2 u[PER / 4]; bf16_t e[PER]; } w;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) w.e[k] = f32_to_bf16(v[k] * inv);
+#pragma unroll
+    for (int k = 0; k < PER / 4; ++k) reinterpret_cast<uint2*>(out)[k] = w.u[k];
+  } else {
+    const long long at = ((long long)part * a.off[a.B] + r0 + rr) * a.Hq + hh;
+    if (d0 == 0) a.part_ml[at] = make_float2(mm, sum);
+    float4* po = reinterpret_cast<float4*>(a.part_o + at * DH + d0);
+#pragma unroll
+    for (int k = 0; k < PER / 4; ++k) po[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+  }
+}
+
+// Joins the parts: out = sum_s f_s o_s / sum_s f_s l_s, f_s = 2^(m_s - max m).
+template <int DH>
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) {
+  constexpr int LPH = DH / 4;  // lanes a row and head
+  const long long item = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH, items = (long long)a.off[a.B] * a.Hq;
+  if (item >= items) return;
+  const int r = static_cast<int>(item / a.Hq), h = static_cast<int>(item - (long long)r * a.Hq), d0 = 4 * (threadIdx.x % LPH);
+  float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_ml[(long long)s * items + item];
+    if (ml.y != 0.0f) mm = fmaxf(mm, ml.x);
+  }
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_ml[(long long)s * items + item];
+    if (ml.y == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+    const float4 o = *reinterpret_cast<const float4*>(a.part_o + ((long long)s * items + item) * DH + d0);
+    sum = fmaf(f, ml.y, sum);
+    v[0] = fmaf(f, o.x, v[0]);
+    v[1] = fmaf(f, o.y, v[1]);
+    v[2] = fmaf(f, o.z, v[2]);
+    v[3] = fmaf(f, o.w, v[3]);
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  union { uint2 u; bf16_t e[4]; } w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w.e[k] = f32_to_bf16(v[k] * inv);
+  *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + r * a.ldo + h * DH + d0) = w.u;
 }
 
 }  // namespace
 
-hipError_t launch_cache_attention(CacheAttnArgs& a, hipStream_t s) {
-  int most = 0;
-  for (int b = 0; b < a.B; ++b) most = max(most, a.off[b + 1] - a.off[b]);
-  const dim3 grid(most, a.Hq, a.B), block(NT);
-  if (a.fp4)
-    return a.Dh == 128 ? launch_kernel("cache_attention", cache_attention_kernel<128, true>, grid, block, 0, s, a)
-                       : launch_kernel("cache_attention", cache_attention_kernel<64, true>, grid, block, 0, s, a);
-  return a.Dh == 128 ? launch_kernel("cache_attention", cache_attention_kernel<128, false>, grid, block, 0, s, a)
-                     : launch_kernel("cache_attention", cache_attention_kernel<64, false>, grid, block, 0, s, a);
+namespace {
+
+// ---------------------------------------------------------------- prompts
+// Workgroup (query block of 32 NW rows, query head, sequence, part of the
+// tokens); wave w owns 32 rows.  64 tokens at a time pass through LDS, two
+// buffers, one barrier a block, the next block on its way under this one's
+// products: bf16 pages by direct loads, 4-bit pages through registers, widened
+// once for all the workgroup's rows.
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+constexpr int kKeys = 64;
+
+__device__ const uint4 zero_piece[1] = {};  // what a hidden token's values are loaded from
+
+// Row and column of accumulator register r of lane `lane` in a 32 x 32 matrix-core block.
+__device__ __forceinline__ int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is written here and nowhere else in the file
+__device__ __forceinline__ void dma16(const void* gsrc, uint32_t m) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gsrc), "s"(m) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Position of 16-byte chunk c of key k's row of K in LDS.
+template <int DH> __device__ __forceinline__ int kchunk(int c, int k) {
+  return DH == 128 ? c ^ (k & 15) : c ^ ((k >> 1) & 7);
+}
+
+template <int DH, bool FP4, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void cache_prompt_kernel(const CacheAttnArgs a) {
+  constexpr int NTH = 64 * NW, ROW = 2 * DH, BUF = kKeys * ROW, CPR = ROW / 16;  // bytes a token, a buffer; pieces a token
+  constexpr int NS = DH / 16, ND = DH / 32;
+  __shared__ __attribute__((aligned(1024))) char lds[4 * BUF];  // K, K, V, V
+  const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
+  const int tiles = gridDim.x / a.splits, part = blockIdx.x % a.splits;
+  const int q0 = (tiles - 1 - static_cast<int>(blockIdx.x) / a.splits) * 32 * NW;  // the longest first
+  if (n <= a.step_rows || q0 >= n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5, h = blockIdx.y, kvh = h / a.G;
+  const int len = cache_len(a.c, b), base = len - n;
+  const int lo = base + q0, hi = base + min(q0 + 32 * NW, n);          // the workgroup's tokens
+  const int wlo = lo + 32 * wave, whi = min(wlo + 32, base + n);       // this wave's (none if whi <= wlo)
+  const int me = wlo + lr, from = a.window > 0 ? me - a.window + 1 : 0;  // this lane's, and its window's first
+  const int from_lo = a.window > 0 ? lo - a.window + 1 : 0;
+  const Blocks blocks = visible_blocks(lo, hi, a.window, a.sinks, kKeys);
+  const int j_begin = static_cast<int>((long long)blocks.count * part / a.splits);
+  const int j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.splits);
+
+  bf16x8_t qf[NS];  // the query's values 16 st + 8 lh + (0..7)
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (r0 + min(q0 + 32 * wave + lr, n - 1)) * a.ldq + h * DH + 8 * lh;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) qf[st] = *reinterpret_cast<const bf16x8_t*>(q + 16 * st);
+  }
+  const uint32_t lds_at = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)&lds[0]));
+  auto seen = [&](int tok) { return static_cast<bool>((tok < hi) & ((tok >= from_lo) | (tok < a.sinks))); };
+
+  uint32_t held = 0;  // bit t: the block on its way has a page for its 16-token tile t
+  constexpr int PIECES = kKeys * DH / 32;                    // 4 bits: 16-byte pieces of K (and of V) a block
+  constexpr int NP = FP4 ? (PIECES + NTH - 1) / NTH : 1;
+  uint4 kp[NP], vp[NP];
+  uint32_t kb[NP], vb[NP];
+  bool vis[NP];
+  auto load = [&](int j) {
+    const int t0 = blocks.token(j, kKeys);
+    long long rows[4];
+    held = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int tok = t0 + 16 * t, page = tok < len ? cache_page(a.c, b, tok) : -1;
+      rows[t] = page >= 0 ? cache_row(a.c, page, kvh, tok) : 0LL;  // (no page: the pool's first tokens, masked)
+      held |= page >= 0 ? 1u << t : 0u;
+    }
+    if constexpr (FP4) {
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        const int e = tid + NTH * u, key = e / (DH / 32), c = e % (DH / 32), t = key >> 4;
+        if (PIECES % NTH != 0 && e >= PIECES) continue;
+        const long long r = (t == 0 ? rows[0] : t == 1 ? rows[1] : t == 2 ? rows[2] : rows[3]) + (key & 15);
+        kp[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * c);
+        vp[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * c);
+        kb[u] = a.c.ks[r * (DH / 32) + c];
+        vb[u] = a.c.vs[r * (DH / 32) + c];
+        vis[u] = ((held >> t) & 1u) && seen(t0 + key);
+      }
+    } else {
+      constexpr int KPI = 64 / CPR, INS = kKeys / KPI / NW;  // keys an instruction, instructions a wave
+#pragma unroll
+      for (int u = 0; u < INS; ++u) {
+        const int k0 = KPI * (wave * INS + u), t = k0 >> 4;  // (uniform)
+        const long long row = (t == 0 ? rows[0] : t == 1 ? rows[1] : t == 2 ? rows[2] : rows[3]) + (k0 & 15);
+        const int key = k0 + lane / CPR, p = lane % CPR;
+        const uint32_t at = lds_at + static_cast<uint32_t>(j & 1) * BUF + 1024u * (wave * INS + u);
+        const long long r = (row + lane / CPR) * ROW;
+        dma16(static_cast<const char*>(a.c.k) + r + 16 * kchunk<DH>(p, key), at);
+        const char* v = static_cast<const char*>(a.c.v) + r + 32 * vchunk<DH>(p >> 1, key) + 16 * (p & 1);
+        dma16(((held >> t) & 1u) && seen(t0 + key) ? v : reinterpret_cast<const char*>(zero_piece), at + 2 * BUF);
+      }
+    }
+  };
+  auto store = [&](int j) {  // 4 bits: the block to LDS, as bf16
+    if constexpr (FP4) {
+      char* kt = lds + (j & 1) * BUF;
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        const int e = tid + NTH * u, key = e / (DH / 32), c = e % (DH / 32);
+        if (PIECES % NTH != 0 && e >= PIECES) continue;
+        const float ks = fp4_scale(kb[u]), vs = fp4_scale(vb[u]);
+        const uint32_t kw[4] = {kp[u].x, kp[u].y, kp[u].z, kp[u].w}, vw[4] = {vp[u].x, vp[u].y, vp[u].z, vp[u].w};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          *reinterpret_cast<uint4*>(kt + key * ROW + 16 * kchunk<DH>(4 * c + x, key)) = fp4_eight(kw[x], ks);
+          const uint4 v = vis[u] ? fp4_eight(vw[x], vs) : make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(kt + 2 * BUF + key * ROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) = v;
+        }
+      }
+    }
+  };
+
+  f32x16_t o[ND];  // O^T: rows 32 d + acc_row = values, column lr = the query
+  float m, l;
+  const float c2 = a.c2;
+  const int tr_key = 4 * lh + ((lane & 15) >> 2);
+  // A first pass takes every value as finite; if a sum comes out infinite or NaN,
+  // a second one keeps such values from the rows that do not see them (their zero
+  // probability would not cancel them): the product runs on the finite values, and
+  // the others add themselves to the rows that see them.
+  auto run = [&](auto careful) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    m = kLow;
+    l = 0.0f;
+    if (j_begin < j_end) load(j_begin);
+    for (int j = j_begin; j < j_end; ++j) {
+      const int cur = blocks.token(j, kKeys);
+      const uint32_t have = held;
+      if constexpr (FP4) store(j);
+      else __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the block
+      __syncthreads();
+      if (j + 1 < j_end) load(j + 1);
+      // nothing of it for this wave (it still loads for the others)
+      if (whi <= wlo || cur >= whi || (a.window > 0 && cur + kKeys <= wlo - a.window + 1 && cur >= a.sinks)) continue;
+      const bool whole = have == 15u && cur + kKeys - 1 <= wlo &&
+                         (a.window == 0 || whi - 1 - cur < a.window || cur + kKeys <= a.sinks);
+      const char* K = lds + (j & 1) * BUF;
+      const char* V = lds + (2 + (j & 1)) * BUF;
+      f32x16_t sc[2];  // S^T: rows = keys 32 t + acc_row, column = the query
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int key = 32 * t + lr;
+          sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              *reinterpret_cast<const bf16x8_t*>(K + key * ROW + 16 * kchunk<DH>(2 * st + lh, key)), qf[st], sc[t], 0, 0, 0);
+        }
+      auto visible = [&](int k) {
+        const int tok = cur + k;
+        return static_cast<bool>(((have >> (k >> 4)) & 1u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
+      };
+      float z[2][16];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[t][r] = sc[t][r];
+      if (!whole) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) z[t][r] = visible(32 * t + acc_row(r, lane)) ? z[t][r] : -INFINITY;
+      }
+      float mx = z[0][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[t][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+      const bool grow = mx > m + kRescale;
+      if (__any(grow)) {
+        const float al = grow ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;  // (first block: 0)
+        if (grow) m = mx;
+        l *= al;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= al;
+      }
+      bf16x8_t pf[4];  // the probabilities of steps of 16 keys
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(z[st >> 1][8 * (st & 1) + k], c2, -m));
+          l += p;
+          pf[st][k] = static_cast<__bf16>(p);
+        }
+      auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
+        const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
+        const int c = 2 * d + ((lane >> 4) & 1);
+        return join(tr_read(at + 32 * vchunk<DH>(c, tr_key)), tr_read(at + 8 * ROW + 32 * vchunk<DH>(c, tr_key + 8)));
+      };
+      if constexpr (!careful.value) {
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfrag(st, d), pf[st], o[d], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(clean8(vfrag(st, d)), pf[st], o[d], 0, 0, 0);
+        for (int k = 0; k < kKeys; ++k) {
+          const bool see = visible(k);
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int dim = 32 * d + acc_row(r, lane);
+              const bf16_t v = *reinterpret_cast<const bf16_t*>(V + k * ROW + 32 * vchunk<DH>(dim >> 4, k) + 2 * (dim & 15));
+              o[d][r] += (see & ((v & 0x7f80) == 0x7f80)) ? bf16_to_f32(v) : 0.0f;
+            }
+        }
+      }
+    }
+    float any = 0.0f;  // NaN once a sum is not finite
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) any = fmaf(o[d][r], 0.0f, any);
+    return __syncthreads_or(any != 0.0f && q0 + 32 * wave + lr < n);  // (and K and V are read out)
+  };
+  if (run(std::false_type{})) run(std::true_type{});
+  if (whi <= wlo) return;
+  l += __shfl_xor(l, 32, 64);
+  const int i = q0 + 32 * wave + lr;  // this lane's row
+  if (a.splits > 1) {
+    if (i >= n) return;
+    const long long at = ((long long)part * a.off[a.B] + r0 + i) * a.Hq + h;
+    if (lh == 0) a.part_ml[at] = make_float2(m, l);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(a.part_o + at * DH + 32 * d + 8 * g + 4 * lh) =
+            make_float4(o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]);
+    return;
+  }
+  // each wave's output rows through LDS, 8 values more apart than they are long
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16_t* ot = reinterpret_cast<bf16_t*>(lds) + wave * 32 * (DH + 8);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      ushort4 w;
+      w.x = f32_to_bf16(o[d][4 * g] * inv);
+      w.y = f32_to_bf16(o[d][4 * g + 1] * inv);
+      w.z = f32_to_bf16(o[d][4 * g + 2] * inv);
+      w.w = f32_to_bf16(o[d][4 * g + 3] * inv);
+      *reinterpret_cast<ushort4*>(ot + lr * (DH + 8) + 32 * d + 8 * g + 4 * lh) = w;
+    }
+  constexpr int LPR = DH / 8, RPI = 64 / LPR;  // lanes a row, rows at a time
+  bf16_t* out = static_cast<bf16_t*>(a.out) + (long long)(r0 + q0 + 32 * wave) * a.ldo + h * DH;
+#pragma unroll
+  for (int u = 0; u < 32 / RPI; ++u) {  // (this wave's own rows: no barrier)
+    const int r = RPI * u + lane / LPR, c = 8 * (lane % LPR);
+    if (q0 + 32 * wave + r < n)
+      *reinterpret_cast<uint4*>(out + (long long)r * a.ldo + c) = *reinterpret_cast<const uint4*>(ot + r * (DH + 8) + c);
+  }
+}
+
+// Sequences of up to so many new rows run on the kernel for few rows: its tiles
+// of 16 (row, head) pairs read the cache once each, n G / 16 times a key/value
+// head, the other kernel once for each of the G heads.
+constexpr int kStepRows = 16;
+
+struct Plan {
+  int step_most, prompt_most;  // the longest of each kind (0: none)
+  int tiles;                   // 16-column tiles of the longest few-row sequence
+  int splits;
+};
+
+}  // namespace
+
+namespace {
+Plan make_plan(const int* off, int B, int Hq, int Hkv, long long tokens, int cus) {
+  Plan p{0, 0, 1, 1};
+  const int G = Hq / Hkv;
+  long long groups = 0;
+  for (int b = 0; b < B; ++b) {
+    const int n = off[b + 1] - off[b];
+    if (n <= kStepRows) {
+      p.step_most = max(p.step_most, n);
+      groups += (long long)((n * G + 15) / 16) * Hkv;
+    } else {
+      p.prompt_most = max(p.prompt_most, n);
+      groups += (long long)((n + 127) / 128) * Hq;
+    }
+  }
+  p.tiles = max(1, (p.step_most * G + 15) / 16);
+  const long long want = 2LL * cus;
+  const long long s = min(min(want / max(groups, 1LL), tokens / 256), 64LL);
+  p.splits = static_cast<int>(max(s, 1LL));
+  return p;
+}
+}  // namespace
+
+// The parts a call is split into, for the workspace (0 floats: none).
+int cache_attention_splits(const int* off, int B, int Hq, int Hkv, long long max_tokens, int cus) {
+  return make_plan(off, B, Hq, Hkv, max_tokens, cus).splits;
+}
+
+hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cus, hipStream_t s) {
+  const Plan p = make_plan(a.off, a.B, a.Hq, a.Hq / a.G, max_tokens, cus);
+  a.splits = p.splits;
+  a.tiles = p.tiles;
+  a.step_rows = kStepRows;
+  hipError_t e = hipSuccess;
+  if (p.step_most > 0) {
+    const dim3 grid(p.splits, a.Hq / a.G * p.tiles, a.B), block(64 * kStepWaves);
+    if (a.fp4)
+      e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, true>, grid, block, 0, s, a)
+                      : launch_kernel("cache_step", cache_step_kernel<64, true>, grid, block, 0, s, a);
+    else
+      e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, false>, grid, block, 0, s, a)
+                      : launch_kernel("cache_step", cache_step_kernel<64, false>, grid, block, 0, s, a);
+  }
+  if (e == hipSuccess && p.prompt_most > 0) {
+    const dim3 grid((p.prompt_most + 127) / 128 * p.splits, a.Hq, a.B), block(256);
+    if (a.fp4)
+      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true, 4>, grid, block, 0, s, a)
+                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, true, 4>, grid, block, 0, s, a);
+    else
+      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false, 4>, grid, block, 0, s, a)
+                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, false, 4>, grid, block, 0, s, a);
+  }
+  if (e == hipSuccess && p.splits > 1) {
+    const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
+    const dim3 grid(static_cast<unsigned>((items + per - 1) / per)), block(256);
+    e = a.Dh == 128 ? launch_kernel("cache_join", cache_join_kernel<128>, grid, block, 0, s, a)
+                    : launch_kernel("cache_join", cache_join_kernel<64>, grid, block, 0, s, a);
+  }
+  return e;
 }
 
 }  // namespace mapk

@@ -474,9 +474,16 @@ struct CacheAttnArgs {
   int B, Hq, G, Dh, window, sinks;
   float c2;               // scale log2(e)
   bool fp4;
+  // set by the launch: parts of the tokens, 16-column tiles of a few-row sequence,
+  // the most rows of one
+  int splits, tiles, step_rows;
+  float* part_o;          // [splits][rows][Hq][Dh] each part's sums, when splits > 1
+  float2* part_ml;        // [splits][rows][Hq] and (m, l)
   int off[MAP_CACHE_MAX_BATCH + 1];
 };
-hipError_t launch_cache_attention(CacheAttnArgs& a, hipStream_t s);
+// Parts that a call is split into (the workspace holds their sums), and the call.
+int cache_attention_splits(const int* off, int B, int Hq, int Hkv, long long max_tokens, int cus);
+hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cus, hipStream_t s);
 
 // ---------------------------------------------------------------- teacher selection
 constexpr int kTeacherMaxLayers = 256;

@@ -1552,6 +1552,22 @@ CachePages cache_pages(const map_cache& c, const int32_t* table, int max_pages, 
   return p;
 }
 
+// The parts' sums of a split attention (at least one byte, so that 0 says invalid).
+struct CacheAttentionWs {
+  float2* ml;
+  float* o;
+};
+
+CacheAttentionWs carve_cache_attention(Carver& w, const map_cache& c, int B, int n_heads, int max_pages,
+                                       const int32_t* off) {
+  const int splits = cache_attention_splits(off, B, n_heads, c.n_kv_heads, (long long)max_pages * c.page, device_cus());
+  const size_t items = splits > 1 ? (size_t)splits * off[B] * n_heads : 0;
+  CacheAttentionWs t;
+  t.ml = w.take<float2>(items + 1);
+  t.o = w.take<float>(items * c.head_dim);
+  return t;
+}
+
 map_status cache_rows_args(CacheRowsArgs& a, const map_cache* c, map_dtype dt, int B, const int32_t* table,
                            int max_pages, const int32_t* len, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            const int32_t* off) {
@@ -1640,7 +1656,9 @@ size_t map_cache_attention_workspace(const map_cache* c, int B, int n_heads, int
   if (!valid_cache(c) || !valid_table(*c, max_pages) || !valid_rows(seq_off_host, B) || n_heads < 1 ||
       n_heads > 1024 || n_heads % c->n_kv_heads != 0)
     return 0;
-  return kAlign;
+  Carver w(nullptr);
+  carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
+  return w.off;
 }
 
 map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_heads, const int32_t* table,
@@ -1672,7 +1690,12 @@ map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_he
   a.c2 = static_cast<float>(scale * 1.4426950408889634);
   a.fp4 = c->type == MAP_CACHE_MXFP4;
   std::copy(seq_off_host, seq_off_host + B + 1, a.off);
-  return hip_status(launch_cache_attention(a, static_cast<hipStream_t>(stream)));
+  Carver w(ws);
+  const CacheAttentionWs t = carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
+  a.part_ml = t.ml;
+  a.part_o = t.o;
+  return hip_status(
+      launch_cache_attention(a, (long long)max_pages * c->page, device_cus(), static_cast<hipStream_t>(stream)));
 }
 
 map_status map_set_finite_check(int enable) {
