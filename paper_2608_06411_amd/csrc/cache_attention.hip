@@ -438,11 +438,11 @@ __global__ __launch_bounds__(64 * NW, 2) void cache_prompt_kernel(const CacheAtt
   constexpr int NS = DH / 16, ND = DH / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * BUF];  // K, K, V, V
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
-  const int tiles = gridDim.x / a.splits, part = blockIdx.x % a.splits;
-  const int q0 = (tiles - 1 - static_cast<int>(blockIdx.x) / a.splits) * 32 * NW;  // the longest first
+  const int tiles = gridDim.y / a.splits, part = blockIdx.y % a.splits;
+  const int q0 = (tiles - 1 - static_cast<int>(blockIdx.y) / a.splits) * 32 * NW;  // the longest first
   if (n <= a.step_rows || q0 >= n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, lh = lane >> 5, h = blockIdx.y, kvh = h / a.G;
+  const int lr = lane & 31, lh = lane >> 5, h = blockIdx.x, kvh = h / a.G;
   const int len = cache_len(a.c, b), base = len - n;
   const int lo = base + q0, hi = base + min(q0 + 32 * NW, n);          // the workgroup's tokens
   const int wlo = lo + 32 * wave, whi = min(wlo + 32, base + n);       // this wave's (none if whi <= wlo)
@@ -736,7 +736,7 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cu
                       : launch_kernel("cache_step", cache_step_kernel<64, false>, grid, block, 0, s, a);
   }
   if (e == hipSuccess && p.prompt_most > 0) {
-    const dim3 grid((p.prompt_most + 127) / 128 * p.splits, a.Hq, a.B), block(256);
+    const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.splits, a.B), block(256);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true, 4>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, true, 4>, grid, block, 0, s, a);
