@@ -33,6 +33,14 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 constexpr float kLow = -3.0e38f;   // m before the first visible score
 constexpr float kRescale = 6.0f;   // log2 of the growth that a row's factor may lag behind
 
+// x in a vector register, whatever the compiler knows of it: a load at x is then one
+// of the vector loads, which a block's wait covers, and not a scalar one, whose
+// return the next LDS read would have to wait for.
+__device__ __forceinline__ int in_vector(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 __device__ __forceinline__ s16x4_t tr_read(const void* p) {
   typedef __attribute__((address_space(3))) s16x4_t lds_t;
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -89,9 +97,10 @@ template <int DH, bool FP4> struct StepShape {
   static constexpr int BYTES = kStepWaves * (KB * VROW > 16 * OLD * 4 ? KB * VROW : 16 * OLD * 4);
 };
 
-// Position of 32-byte chunk c of key k's row in LDS (16 keys' chunks spread over all banks).
+// Position of 32-byte chunk c of key k's row of V in LDS: the 32 lanes of half a
+// transposing read (8 keys' one chunk, or 4 keys' two) name all 64 banks once.
 template <int DH> __device__ __forceinline__ int vchunk(int c, int k) {
-  return DH == 128 ? c ^ (k & 7) : c ^ ((k >> 1) & 3);
+  return DH == 128 ? c ^ (((k & 3) << 1) | ((k >> 2) & 1)) : c ^ ((k & 2) | ((k >> 2) & 1));
 }
 
 template <int DH, bool FP4>
@@ -407,11 +416,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) 
 namespace {
 
 // ---------------------------------------------------------------- prompts
-// Workgroup (query block of 32 NW rows, query head, sequence, part of the
-// tokens); wave w owns 32 rows.  64 tokens at a time pass through LDS, two
-// buffers, one barrier a block, the next block on its way under this one's
-// products: bf16 pages by direct loads, 4-bit pages through registers, widened
-// once for all the workgroup's rows.
+// Workgroup (query block of 128 rows, query head, sequence, part of the tokens);
+// wave w owns 32 rows.  64 tokens at a time pass through LDS, two buffers, one
+// barrier a block, the next block on its way under this one's products: bf16
+// pages by direct loads, 4-bit pages through registers, widened once for all the
+// workgroup's rows.  A wave brings the 16 tokens that one table entry names, and
+// has that entry read a block before.
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 constexpr int kKeys = 64;
 
@@ -432,11 +442,12 @@ template <int DH> __device__ __forceinline__ int kchunk(int c, int k) {
   return DH == 128 ? c ^ (k & 15) : c ^ ((k >> 1) & 7);
 }
 
-template <int DH, bool FP4, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void cache_prompt_kernel(const CacheAttnArgs a) {
-  constexpr int NTH = 64 * NW, ROW = 2 * DH, BUF = kKeys * ROW, CPR = ROW / 16;  // bytes a token, a buffer; pieces a token
+template <int DH, bool FP4>
+__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArgs a) {
+  constexpr int NW = 4, NTH = 64 * NW, ROW = 2 * DH, BUF = kKeys * ROW, CPR = ROW / 16;  // bytes a token, a buffer; pieces a token
   constexpr int NS = DH / 16, ND = DH / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * BUF];  // K, K, V, V
+  __shared__ __attribute__((aligned(16))) int have_page[2][NW];  // which of a block's four 16-token tiles have a page
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
   const int tiles = gridDim.y / a.splits, part = blockIdx.y % a.splits;
   const int q0 = (tiles - 1 - static_cast<int>(blockIdx.y) / a.splits) * 32 * NW;  // the longest first
@@ -462,62 +473,55 @@ __global__ __launch_bounds__(64 * NW, 2) void cache_prompt_kernel(const CacheAtt
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)&lds[0]));
   auto seen = [&](int tok) { return static_cast<bool>((tok < hi) & ((tok >= from_lo) | (tok < a.sinks))); };
 
-  uint32_t held = 0;  // bit t: the block on its way has a page for its 16-token tile t
-  constexpr int PIECES = kKeys * DH / 32;                    // 4 bits: 16-byte pieces of K (and of V) a block
-  constexpr int NP = FP4 ? (PIECES + NTH - 1) / NTH : 1;
-  uint4 kp[NP], vp[NP];
-  uint32_t kb[NP], vb[NP];
-  bool vis[NP];
-  auto load = [&](int j) {
-    const int t0 = blocks.token(j, kKeys);
-    long long rows[4];
-    held = 0;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int tok = t0 + 16 * t, page = tok < len ? cache_page(a.c, b, tok) : -1;
-      rows[t] = page >= 0 ? cache_row(a.c, page, kvh, tok) : 0LL;  // (no page: the pool's first tokens, masked)
-      held |= page >= 0 ? 1u << t : 0u;
-    }
+  // Each wave brings 16 of a block's 64 tokens, so one table entry a block.
+  constexpr int PPK = FP4 ? DH / 32 : CPR;          // 16-byte pieces a token in a page
+  constexpr int NP = FP4 ? 1 : 16 * PPK / 64;       // pieces a lane, of keys and of values
+  const int mine = 16 * wave;
+  auto entry = [&](int j) {  // the table's word for this wave's tokens of block j
+    const int tok = blocks.token(j, kKeys) + mine;
+    const int* at = a.c.table + (long long)b * a.c.max_pages;
+    return j < j_end && tok < len ? at[in_vector(tok >> a.c.shift)] : -1;
+  };
+  uint4 kp, vp;  // 4 bits: the piece on its way
+  uint32_t kb, vb;
+  bool vis;
+  auto load = [&](int j, int ent) {
+    const int t0 = blocks.token(j, kKeys), page = __builtin_amdgcn_readfirstlane(ent);
+    const bool has = static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages);
+    const long long row = has ? cache_row(a.c, page, kvh, t0 + mine) : 0LL;  // (no page: the pool's first tokens, masked)
+    if (lane == 0) have_page[j & 1][wave] = has ? 1 : 0;
     if constexpr (FP4) {
+      const int key = lane / PPK % 16, c = lane % PPK;
+      const long long r = row + key;
+      kp = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * c);
+      vp = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * c);
+      kb = a.c.ks[r * PPK + c];
+      vb = a.c.vs[r * PPK + c];
+      vis = has && seen(t0 + mine + key);
+    } else {
+      constexpr int KPI = 64 / CPR;  // keys an instruction
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
-        const int e = tid + NTH * u, key = e / (DH / 32), c = e % (DH / 32), t = key >> 4;
-        if (PIECES % NTH != 0 && e >= PIECES) continue;
-        const long long r = (t == 0 ? rows[0] : t == 1 ? rows[1] : t == 2 ? rows[2] : rows[3]) + (key & 15);
-        kp[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * c);
-        vp[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * c);
-        kb[u] = a.c.ks[r * (DH / 32) + c];
-        vb[u] = a.c.vs[r * (DH / 32) + c];
-        vis[u] = ((held >> t) & 1u) && seen(t0 + key);
-      }
-    } else {
-      constexpr int KPI = 64 / CPR, INS = kKeys / KPI / NW;  // keys an instruction, instructions a wave
-#pragma unroll
-      for (int u = 0; u < INS; ++u) {
-        const int k0 = KPI * (wave * INS + u), t = k0 >> 4;  // (uniform)
-        const long long row = (t == 0 ? rows[0] : t == 1 ? rows[1] : t == 2 ? rows[2] : rows[3]) + (k0 & 15);
-        const int key = k0 + lane / CPR, p = lane % CPR;
-        const uint32_t at = lds_at + static_cast<uint32_t>(j & 1) * BUF + 1024u * (wave * INS + u);
-        const long long r = (row + lane / CPR) * ROW;
+        const int key = mine + KPI * u + lane / CPR, p = lane % CPR;
+        const uint32_t at = lds_at + static_cast<uint32_t>(j & 1) * BUF + 1024u * (wave * NP + u);
+        const long long r = (row + KPI * u + lane / CPR) * ROW;
         dma16(static_cast<const char*>(a.c.k) + r + 16 * kchunk<DH>(p, key), at);
         const char* v = static_cast<const char*>(a.c.v) + r + 32 * vchunk<DH>(p >> 1, key) + 16 * (p & 1);
-        dma16(((held >> t) & 1u) && seen(t0 + key) ? v : reinterpret_cast<const char*>(zero_piece), at + 2 * BUF);
+        dma16(has && seen(t0 + key) ? v : reinterpret_cast<const char*>(zero_piece), at + 2 * BUF);
       }
     }
   };
-  auto store = [&](int j) {  // 4 bits: the block to LDS, as bf16
+  auto store = [&](int j) {  // 4 bits: the piece to LDS, as bf16
     if constexpr (FP4) {
       char* kt = lds + (j & 1) * BUF;
-#pragma unroll
-      for (int u = 0; u < NP; ++u) {
-        const int e = tid + NTH * u, key = e / (DH / 32), c = e % (DH / 32);
-        if (PIECES % NTH != 0 && e >= PIECES) continue;
-        const float ks = fp4_scale(kb[u]), vs = fp4_scale(vb[u]);
-        const uint32_t kw[4] = {kp[u].x, kp[u].y, kp[u].z, kp[u].w}, vw[4] = {vp[u].x, vp[u].y, vp[u].z, vp[u].w};
+      const int key = mine + lane / PPK % 16, c = lane % PPK;
+      const float ks = fp4_scale(kb), vs = fp4_scale(vb);
+      const uint32_t kw[4] = {kp.x, kp.y, kp.z, kp.w}, vw[4] = {vp.x, vp.y, vp.z, vp.w};
+      if (PPK == 4 || lane < 16 * PPK) {  // (head_dim 64: 32 lanes hold the 16 tokens, the others repeat them)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           *reinterpret_cast<uint4*>(kt + key * ROW + 16 * kchunk<DH>(4 * c + x, key)) = fp4_eight(kw[x], ks);
-          const uint4 v = vis[u] ? fp4_eight(vw[x], vs) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 v = vis ? fp4_eight(vw[x], vs) : make_uint4(0u, 0u, 0u, 0u);
           *reinterpret_cast<uint4*>(kt + 2 * BUF + key * ROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) = v;
         }
       }
@@ -539,14 +543,18 @@ __global__ __launch_bounds__(64 * NW, 2) void cache_prompt_kernel(const CacheAtt
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     m = kLow;
     l = 0.0f;
-    if (j_begin < j_end) load(j_begin);
+    int ent = entry(j_begin);
+    if (j_begin < j_end) load(j_begin, ent);
+    ent = entry(j_begin + 1);
     for (int j = j_begin; j < j_end; ++j) {
       const int cur = blocks.token(j, kKeys);
-      const uint32_t have = held;
       if constexpr (FP4) store(j);
       else __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the block
       __syncthreads();
-      if (j + 1 < j_end) load(j + 1);
+      const int4 hp = *reinterpret_cast<const int4*>(have_page[j & 1]);
+      if (j + 1 < j_end) load(j + 1, ent);
+      ent = entry(j + 2);
+      const uint32_t have = __builtin_amdgcn_readfirstlane(hp.x | (hp.y << 1) | (hp.z << 2) | (hp.w << 3));
       // nothing of it for this wave (it still loads for the others)
       if (whi <= wlo || cur >= whi || (a.window > 0 && cur + kKeys <= wlo - a.window + 1 && cur >= a.sinks)) continue;
       const bool whole = have == 15u && cur + kKeys - 1 <= wlo &&
@@ -738,11 +746,11 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cu
   if (e == hipSuccess && p.prompt_most > 0) {
     const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.splits, a.B), block(256);
     if (a.fp4)
-      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true, 4>, grid, block, 0, s, a)
-                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, true, 4>, grid, block, 0, s, a);
+      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true>, grid, block, 0, s, a)
+                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, true>, grid, block, 0, s, a);
     else
-      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false, 4>, grid, block, 0, s, a)
-                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, false, 4>, grid, block, 0, s, a);
+      e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false>, grid, block, 0, s, a)
+                      : launch_kernel("cache_prompt", cache_prompt_kernel<64, false>, grid, block, 0, s, a);
   }
   if (e == hipSuccess && p.splits > 1) {
     const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
