@@ -33,12 +33,10 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 constexpr float kLow = -3.0e38f;   // m before the first visible score
 constexpr float kRescale = 6.0f;   // log2 of the growth that a row's factor may lag behind
 
-// x in a vector register, whatever the compiler knows of it: a load at x is then one
-// of the vector loads, which a block's wait covers, and not a scalar one, whose
-// return the next LDS read would have to wait for.
-__device__ __forceinline__ int in_vector(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
+// The larger of lanes l and l ^ 32, in both.
+__device__ __forceinline__ float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 __device__ __forceinline__ s16x4_t tr_read(const void* p) {
@@ -435,6 +433,10 @@ __device__ __forceinline__ int acc_row(int r, int lane) { return 8 * (r >> 2) + 
 __device__ __forceinline__ void dma16(const void* gsrc, uint32_t m) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gsrc), "s"(m) : "memory", "m0");
 }
+// The same with one base address for the wave and an offset a lane.
+__device__ __forceinline__ void dma16_from(const void* base, uint32_t off, uint32_t m) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(m) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // Position of 16-byte chunk c of key k's row of K in LDS.
@@ -444,10 +446,10 @@ template <int DH> __device__ __forceinline__ int kchunk(int c, int k) {
 
 template <int DH, bool FP4>
 __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArgs a) {
-  constexpr int NW = 4, NTH = 64 * NW, ROW = 2 * DH, BUF = kKeys * ROW, CPR = ROW / 16;  // bytes a token, a buffer; pieces a token
+  constexpr int NW = 4, ROW = 2 * DH, BUF = kKeys * ROW, CPR = ROW / 16;  // bytes a token, a buffer; pieces a token
   constexpr int NS = DH / 16, ND = DH / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * BUF];  // K, K, V, V
-  __shared__ __attribute__((aligned(16))) int have_page[2][NW];  // which of a block's four 16-token tiles have a page
+  __shared__ int4 pages[256];
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
   const int tiles = gridDim.y / a.splits, part = blockIdx.y % a.splits;
   const int q0 = (tiles - 1 - static_cast<int>(blockIdx.y) / a.splits) * 32 * NW;  // the longest first
@@ -473,67 +475,204 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)&lds[0]));
   auto seen = [&](int tok) { return static_cast<bool>((tok < hi) & ((tok >= from_lo) | (tok < a.sinks))); };
 
-  // Each wave brings 16 of a block's 64 tokens, so one table entry a block.
+  // The pages of up to 256 blocks at a time, four 16-token tiles each (-1: none), in LDS.
+  auto fill_pages = [&](int j) {
+    const int t0 = j + tid < j_end ? blocks.token(j + tid, kKeys) : len;
+    int4 e;
+    e.x = t0 < len ? cache_page(a.c, b, t0) : -1;
+    e.y = t0 + 16 < len ? cache_page(a.c, b, t0 + 16) : -1;
+    e.z = t0 + 32 < len ? cache_page(a.c, b, t0 + 32) : -1;
+    e.w = t0 + 48 < len ? cache_page(a.c, b, t0 + 48) : -1;
+    pages[tid] = e;
+  };
+  // Each wave brings 16 of a block's 64 tokens.
   constexpr int PPK = FP4 ? DH / 32 : CPR;          // 16-byte pieces a token in a page
   constexpr int NP = FP4 ? 1 : 16 * PPK / 64;       // pieces a lane, of keys and of values
+  constexpr int KPI = FP4 ? 16 : 64 / CPR;          // tokens a piece of all lanes covers
   const int mine = 16 * wave;
-  auto entry = [&](int j) {  // the table's word for this wave's tokens of block j
-    const int tok = blocks.token(j, kKeys) + mine;
-    const int* at = a.c.table + (long long)b * a.c.max_pages;
-    return j < j_end && tok < len ? at[in_vector(tok >> a.c.shift)] : -1;
+  uint4 piece;  // 4 bits: the piece on its way
+  uint32_t byte = 0;
+  bool vis = false;
+  long long row = 0;  // row of this wave's first token of the block that comes next, if it has a page
+  bool has = false;
+  uint32_t k_have = 0, have = 0;   // bit t: tile t of that block, of the one at hand, has a page
+  auto find = [&](int j) {  // a tile without a page reads the pool's first tokens, masked
+    const int4 e = pages[(j - j_begin) & 255];
+    const int own = wave == 0 ? e.x : wave == 1 ? e.y : wave == 2 ? e.z : e.w;
+    const int page = __builtin_amdgcn_readfirstlane(j < j_end ? own : -1);
+    k_have = __builtin_amdgcn_readfirstlane((e.x >= 0 ? 1 : 0) | (e.y >= 0 ? 2 : 0) | (e.z >= 0 ? 4 : 0) | (e.w >= 0 ? 8 : 0));
+    has = page >= 0;
+    row = has ? cache_row(a.c, page, kvh, blocks.token(j, kKeys) + mine) : 0LL;
   };
-  uint4 kp, vp;  // 4 bits: the piece on its way
-  uint32_t kb, vb;
-  bool vis;
-  auto load = [&](int j, int ent) {
-    const int t0 = blocks.token(j, kKeys), page = __builtin_amdgcn_readfirstlane(ent);
-    const bool has = static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages);
-    const long long row = has ? cache_row(a.c, page, kvh, t0 + mine) : 0LL;  // (no page: the pool's first tokens, masked)
-    if (lane == 0) have_page[j & 1][wave] = has ? 1 : 0;
+  const int p_key = FP4 ? lane / PPK % 16 : lane / CPR, p_at = FP4 ? lane % PPK : lane % CPR;
+  auto load_k = [&](int j) {
     if constexpr (FP4) {
-      const int key = lane / PPK % 16, c = lane % PPK;
-      const long long r = row + key;
-      kp = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * c);
-      vp = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * c);
-      kb = a.c.ks[r * PPK + c];
-      vb = a.c.vs[r * PPK + c];
-      vis = has && seen(t0 + mine + key);
+      const long long r = row + p_key;
+      piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * p_at);
+      byte = a.c.ks[r * PPK + p_at];
     } else {
-      constexpr int KPI = 64 / CPR;  // keys an instruction
 #pragma unroll
-      for (int u = 0; u < NP; ++u) {
-        const int key = mine + KPI * u + lane / CPR, p = lane % CPR;
-        const uint32_t at = lds_at + static_cast<uint32_t>(j & 1) * BUF + 1024u * (wave * NP + u);
-        const long long r = (row + KPI * u + lane / CPR) * ROW;
-        dma16(static_cast<const char*>(a.c.k) + r + 16 * kchunk<DH>(p, key), at);
-        const char* v = static_cast<const char*>(a.c.v) + r + 32 * vchunk<DH>(p >> 1, key) + 16 * (p & 1);
-        dma16(has && seen(t0 + key) ? v : reinterpret_cast<const char*>(zero_piece), at + 2 * BUF);
-      }
+      for (int u = 0; u < NP; ++u)
+        dma16_from(static_cast<const char*>(a.c.k) + row * ROW,
+                   (KPI * u + p_key) * ROW + 16 * kchunk<DH>(p_at, KPI * u + p_key),
+                   lds_at + static_cast<uint32_t>(j & 1) * BUF + 1024u * (wave * NP + u));
     }
   };
-  auto store = [&](int j) {  // 4 bits: the piece to LDS, as bf16
+  auto load_v = [&](int j) {
+    const int t0 = blocks.token(j, kKeys) + mine;
     if constexpr (FP4) {
-      char* kt = lds + (j & 1) * BUF;
-      const int key = mine + lane / PPK % 16, c = lane % PPK;
-      const float ks = fp4_scale(kb), vs = fp4_scale(vb);
-      const uint32_t kw[4] = {kp.x, kp.y, kp.z, kp.w}, vw[4] = {vp.x, vp.y, vp.z, vp.w};
-      if (PPK == 4 || lane < 16 * PPK) {  // (head_dim 64: 32 lanes hold the 16 tokens, the others repeat them)
+      const long long r = row + p_key;
+      piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * p_at);
+      byte = a.c.vs[r * PPK + p_at];
+      vis = has & seen(t0 + p_key);
+    } else {
+      const char* base = static_cast<const char*>(a.c.v) + row * ROW;
+      const uint32_t to = lds_at + static_cast<uint32_t>(2 + (j & 1)) * BUF + 1024u * (wave * NP);
+      if (has & (t0 + 15 < hi) & ((t0 >= from_lo) | (t0 + 15 < a.sinks))) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          *reinterpret_cast<uint4*>(kt + key * ROW + 16 * kchunk<DH>(4 * c + x, key)) = fp4_eight(kw[x], ks);
-          const uint4 v = vis ? fp4_eight(vw[x], vs) : make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(kt + 2 * BUF + key * ROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) = v;
+        for (int u = 0; u < NP; ++u)
+          dma16_from(base, (KPI * u + p_key) * ROW + 32 * vchunk<DH>(p_at >> 1, KPI * u + p_key) + 16 * (p_at & 1), to + 1024u * u);
+      } else {  // a token that no row of the workgroup sees: zeros, whatever its values are
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          const int key = KPI * u + p_key;
+          const char* v = base + key * ROW + 32 * vchunk<DH>(p_at >> 1, key) + 16 * (p_at & 1);
+          dma16((has & seen(t0 + key)) ? v : reinterpret_cast<const char*>(zero_piece), to + 1024u * u);
         }
       }
     }
   };
+  // 4 bits: the piece to LDS, as bf16 (head_dim 64: 32 lanes hold the 16 tokens, the others repeat them)
+  auto store_k = [&](int j) {
+    const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+    char* at = lds + (j & 1) * BUF + (mine + p_key) * ROW;
+    if (PPK == 4 || lane < 16 * PPK)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<uint4*>(at + 16 * kchunk<DH>(4 * p_at + x, mine + p_key)) = fp4_eight(w[x], fp4_scale(byte));
+  };
+  auto store_v = [&](int j) {
+    const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+    char* at = lds + (2 + (j & 1)) * BUF + (mine + p_key) * ROW;
+    if (PPK == 4 || lane < 16 * PPK)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<uint4*>(at + 32 * vchunk<DH>(2 * p_at + (x >> 1), mine + p_key) + 16 * (x & 1)) =
+            vis ? fp4_eight(w[x], fp4_scale(byte)) : make_uint4(0u, 0u, 0u, 0u);
+  };
+  // All of this wave's loads but the last NP are here, and every wave's are.
+  auto meet = [&]() {
+    if constexpr (FP4) __syncthreads();
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(NP) : "memory");
+  };
+
+  // The halves of blocks (32 tokens) in which this wave has something to see, as
+  // positions in the run: ia .. ib - 1 (the few hidden ones between the first
+  // tokens and the window are run, masked).
+  int ia = 2 * j_end, ib = 2 * j_begin;
+  if (whi > max(wlo, 0)) {
+    const int shift = 2 * (blocks.sink - blocks.first), ft = a.window > 0 ? max(0, wlo - a.window + 1) : 0;
+    ia = a.window > 0 && blocks.token(j_begin, kKeys) < a.sinks ? 2 * j_begin : max(2 * j_begin, shift + ft / 32);
+    ib = min(2 * j_end, shift + (whi - 1) / 32 + 1);
+  }
 
   f32x16_t o[ND];  // O^T: rows 32 d + acc_row = values, column lr = the query
   float m, l;
   const float c2 = a.c2;
   const int tr_key = 4 * lh + ((lane & 15) >> 2);
-  // A first pass takes every value as finite; if a sum comes out infinite or NaN,
-  // a second one keeps such values from the rows that do not see them (their zero
+  auto token_of = [&](int i) { return blocks.token(i >> 1, kKeys) + 32 * (i & 1); };
+  // S^T of half i: rows = keys acc_row, column = the query
+  auto scores = [&](int i, f32x16_t& sc) {
+    const char* K = lds + ((i >> 1) & 1) * BUF + 32 * (i & 1) * ROW;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          *reinterpret_cast<const bf16x8_t*>(K + lr * ROW + 16 * kchunk<DH>(2 * st + lh, lr)), qf[st], sc, 0, 0, 0);
+  };
+  // Half i's scores masked where its tokens are not all seen, and the row's factor.
+  auto visible = [&](int cur, uint32_t two, int k) {
+    const int tok = cur + k;
+    return static_cast<bool>(((two >> (k >> 4)) & 1u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
+  };
+  auto statistics = [&](int i, f32x16_t& sc) {
+    const int cur = token_of(i);
+    const uint32_t two = (have >> (2 * (i & 1))) & 3u;
+    const bool whole = two == 3u && cur + 31 <= wlo && (a.window == 0 || whi - 1 - cur < a.window || cur + 32 <= a.sinks);
+    if (!whole) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = visible(cur, two, acc_row(r, lane)) ? sc[r] : -INFINITY;
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    mx = max_of_halves(mx) * c2;
+    const bool grow = mx > m + kRescale;
+    if (__any(grow)) {
+      const float al = grow ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;  // (first block: 0)
+      if (grow) m = mx;
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= al;
+    }
+  };
+  // O^T += V^T P^T of half i
+  auto gather = [&](int i, const f32x16_t& sc, auto careful) {
+    const char* V = lds + (2 + ((i >> 1) & 1)) * BUF + 32 * (i & 1) * ROW;
+    auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
+      const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
+      const int c = 2 * d + ((lane >> 4) & 1);
+      return join(tr_read(at + 32 * vchunk<DH>(c, tr_key)), tr_read(at + 8 * ROW + 32 * vchunk<DH>(c, tr_key + 8)));
+    };
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      bf16x8_t pf;  // the probabilities of 16 keys
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
+        l += p;
+        pf[k] = static_cast<__bf16>(p);
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        bf16x8_t v = vfrag(st, d);
+        if constexpr (careful.value) v = clean8(v);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf, o[d], 0, 0, 0);
+      }
+    }
+    if constexpr (careful.value) {
+      const int cur = token_of(i);
+      const uint32_t two = (have >> (2 * (i & 1))) & 3u;
+      for (int k = 0; k < 32; ++k) {
+        const bool see = visible(cur, two, k);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int dim = 32 * d + acc_row(r, lane);
+            const bf16_t v = *reinterpret_cast<const bf16_t*>(V + k * ROW + 32 * vchunk<DH>(dim >> 4, k) + 2 * (dim & 15));
+            o[d][r] += (see & ((v & 0x7f80) == 0x7f80)) ? bf16_to_f32(v) : 0.0f;
+          }
+      }
+    }
+  };
+  // Step i forms half i + 1's scores beside half i's probabilities and sums, so that
+  // the matrix cores have work under the exponentials.  Keys of block j are read in
+  // steps 2 j - 1 and 2 j, its values in steps 2 j and 2 j + 1: an odd step brings
+  // the keys of the block after next, an even one the next block's values, each
+  // with two steps to arrive.
+  auto step = [&](int i, f32x16_t& sc, f32x16_t& next, auto careful) {
+    if (i >= ia && i < ib) {
+      statistics(i, sc);
+      scores(i + 1, next);  // (behind the wave's last half: unused)
+      gather(i, sc, careful);
+    } else if (i + 1 == ia) {
+      scores(i + 1, next);
+    }
+  };
+  // A first run takes every value as finite; if a sum comes out infinite or NaN, a
+  // second one keeps such values from the rows that do not see them (their zero
   // probability would not cancel them): the product runs on the finite values, and
   // the others add themselves to the rows that see them.
   auto run = [&](auto careful) {
@@ -543,101 +682,34 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     m = kLow;
     l = 0.0f;
-    int ent = entry(j_begin);
-    if (j_begin < j_end) load(j_begin, ent);
-    ent = entry(j_begin + 1);
-    for (int j = j_begin; j < j_end; ++j) {
-      const int cur = blocks.token(j, kKeys);
-      if constexpr (FP4) store(j);
-      else __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the block
+    f32x16_t even, odd;
+    if (j_begin < j_end) {
+      fill_pages(j_begin);
       __syncthreads();
-      const int4 hp = *reinterpret_cast<const int4*>(have_page[j & 1]);
-      if (j + 1 < j_end) load(j + 1, ent);
-      ent = entry(j + 2);
-      const uint32_t have = __builtin_amdgcn_readfirstlane(hp.x | (hp.y << 1) | (hp.z << 2) | (hp.w << 3));
-      // nothing of it for this wave (it still loads for the others)
-      if (whi <= wlo || cur >= whi || (a.window > 0 && cur + kKeys <= wlo - a.window + 1 && cur >= a.sinks)) continue;
-      const bool whole = have == 15u && cur + kKeys - 1 <= wlo &&
-                         (a.window == 0 || whi - 1 - cur < a.window || cur + kKeys <= a.sinks);
-      const char* K = lds + (j & 1) * BUF;
-      const char* V = lds + (2 + (j & 1)) * BUF;
-      f32x16_t sc[2];  // S^T: rows = keys 32 t + acc_row, column = the query
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < NS; ++st)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int key = 32 * t + lr;
-          sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              *reinterpret_cast<const bf16x8_t*>(K + key * ROW + 16 * kchunk<DH>(2 * st + lh, key)), qf[st], sc[t], 0, 0, 0);
+      find(j_begin);
+      load_k(j_begin);
+      if constexpr (FP4) store_k(j_begin);
+      load_v(j_begin);
+      if constexpr (FP4) store_v(j_begin);
+      for (int j = j_begin - 1; j < j_end; ++j) {
+        if (j >= j_begin) {  // step 2 j
+          meet();
+          load_v(j + 1);  // (past the last block: the pool's first tokens, unused)
+          step(2 * j, even, odd, careful);
+          if constexpr (FP4) store_v(j + 1);
         }
-      auto visible = [&](int k) {
-        const int tok = cur + k;
-        return static_cast<bool>(((have >> (k >> 4)) & 1u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
-      };
-      float z[2][16];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) z[t][r] = sc[t][r];
-      if (!whole) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) z[t][r] = visible(32 * t + acc_row(r, lane)) ? z[t][r] : -INFINITY;
-      }
-      float mx = z[0][0];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[t][r]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
-      const bool grow = mx > m + kRescale;
-      if (__any(grow)) {
-        const float al = grow ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;  // (first block: 0)
-        if (grow) m = mx;
-        l *= al;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] *= al;
-      }
-      bf16x8_t pf[4];  // the probabilities of steps of 16 keys
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(z[st >> 1][8 * (st & 1) + k], c2, -m));
-          l += p;
-          pf[st][k] = static_cast<__bf16>(p);
+        // step 2 j + 1
+        meet();
+        if (((j + 2 - j_begin) & 255) == 0) {
+          fill_pages(j + 2);
+          __syncthreads();
         }
-      auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
-        const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
-        const int c = 2 * d + ((lane >> 4) & 1);
-        return join(tr_read(at + 32 * vchunk<DH>(c, tr_key)), tr_read(at + 8 * ROW + 32 * vchunk<DH>(c, tr_key + 8)));
-      };
-      if constexpr (!careful.value) {
-#pragma unroll
-        for (int st = 0; st < 4; ++st)
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfrag(st, d), pf[st], o[d], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int st = 0; st < 4; ++st)
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(clean8(vfrag(st, d)), pf[st], o[d], 0, 0, 0);
-        for (int k = 0; k < kKeys; ++k) {
-          const bool see = visible(k);
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int dim = 32 * d + acc_row(r, lane);
-              const bf16_t v = *reinterpret_cast<const bf16_t*>(V + k * ROW + 32 * vchunk<DH>(dim >> 4, k) + 2 * (dim & 15));
-              o[d][r] += (see & ((v & 0x7f80) == 0x7f80)) ? bf16_to_f32(v) : 0.0f;
-            }
-        }
+        const uint32_t h = k_have;  // of block j + 1
+        find(j + 2);
+        load_k(j + 2);
+        step(2 * j + 1, odd, even, careful);
+        if constexpr (FP4) store_k(j + 2);
+        have = h;
       }
     }
     float any = 0.0f;  // NaN once a sum is not finite
@@ -645,6 +717,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) any = fmaf(o[d][r], 0.0f, any);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing on its way to LDS
     return __syncthreads_or(any != 0.0f && q0 + 32 * wave + lr < n);  // (and K and V are read out)
   };
   if (run(std::false_type{})) run(std::true_type{});
