@@ -470,6 +470,10 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     const bf16_t* q = static_cast<const bf16_t*>(a.q) + (r0 + min(q0 + 32 * wave + lr, n - 1)) * a.ldq + h * DH + 8 * lh;
 #pragma unroll
     for (int st = 0; st < NS; ++st) qf[st] = *reinterpret_cast<const bf16x8_t*>(q + 16 * st);
+    // The queries are waited for here: left to their first use, inside the loop, the
+    // compiler's waits for them would take in every block on its way to LDS.
+#pragma unroll
+    for (int st = 0; st < NS; ++st) asm volatile("" : "+v"(qf[st]));
   }
   const uint32_t lds_at = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)&lds[0]));
