@@ -494,17 +494,20 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   constexpr int NP = FP4 ? 1 : 16 * PPK / 64;       // pieces a lane, of keys and of values
   constexpr int KPI = FP4 ? 16 : 64 / CPR;          // tokens a piece of all lanes covers
   const int mine = 16 * wave;
-  uint4 piece;  // 4 bits: the piece on its way
-  uint32_t byte = 0;
+  uint4 k_piece, v_piece;  // 4 bits: the pieces on their way
+  uint32_t k_byte = 0, v_byte = 0;
   bool vis = false;
-  long long row = 0;  // row of this wave's first token of the block that comes next, if it has a page
-  bool has = false;
-  uint32_t k_have = 0, have = 0;   // bit t: tile t of that block, of the one at hand, has a page
+  long long row = 0, v_row = 0;  // rows of this wave's first token of the blocks whose keys, values come next,
+  bool has = false, v_has = false;  // and whether it has a page
+  uint32_t have = 0;  // four bits for each of the last blocks found, the latest lowest: which 16-token tiles have a page
   auto find = [&](int j) {  // a tile without a page reads the pool's first tokens, masked
     const int4 e = pages[(j - j_begin) & 255];
     const int own = wave == 0 ? e.x : wave == 1 ? e.y : wave == 2 ? e.z : e.w;
     const int page = __builtin_amdgcn_readfirstlane(j < j_end ? own : -1);
-    k_have = __builtin_amdgcn_readfirstlane((e.x >= 0 ? 1 : 0) | (e.y >= 0 ? 2 : 0) | (e.z >= 0 ? 4 : 0) | (e.w >= 0 ? 8 : 0));
+    have = (have << 4) |
+           __builtin_amdgcn_readfirstlane((e.x >= 0 ? 1 : 0) | (e.y >= 0 ? 2 : 0) | (e.z >= 0 ? 4 : 0) | (e.w >= 0 ? 8 : 0));
+    v_row = row;
+    v_has = has;
     has = page >= 0;
     row = has ? cache_row(a.c, page, kvh, blocks.token(j, kKeys) + mine) : 0LL;
   };
@@ -512,8 +515,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   auto load_k = [&](int j) {
     if constexpr (FP4) {
       const long long r = row + p_key;
-      piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * p_at);
-      byte = a.c.ks[r * PPK + p_at];
+      k_piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.k) + r * (DH / 2) + 16 * p_at);
+      k_byte = a.c.ks[r * PPK + p_at];
     } else {
 #pragma unroll
       for (int u = 0; u < NP; ++u)
@@ -525,14 +528,14 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   auto load_v = [&](int j) {
     const int t0 = blocks.token(j, kKeys) + mine;
     if constexpr (FP4) {
-      const long long r = row + p_key;
-      piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * p_at);
-      byte = a.c.vs[r * PPK + p_at];
-      vis = has & seen(t0 + p_key);
+      const long long r = v_row + p_key;
+      v_piece = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * (DH / 2) + 16 * p_at);
+      v_byte = a.c.vs[r * PPK + p_at];
+      vis = v_has & seen(t0 + p_key);
     } else {
-      const char* base = static_cast<const char*>(a.c.v) + row * ROW;
+      const char* base = static_cast<const char*>(a.c.v) + v_row * ROW;
       const uint32_t to = lds_at + static_cast<uint32_t>(2 + (j & 1)) * BUF + 1024u * (wave * NP);
-      if (has & (t0 + 15 < hi) & ((t0 >= from_lo) | (t0 + 15 < a.sinks))) {
+      if (v_has & (t0 + 15 < hi) & ((t0 >= from_lo) | (t0 + 15 < a.sinks))) {
 #pragma unroll
         for (int u = 0; u < NP; ++u)
           dma16_from(base, (KPI * u + p_key) * ROW + 32 * vchunk<DH>(p_at >> 1, KPI * u + p_key) + 16 * (p_at & 1), to + 1024u * u);
@@ -541,44 +544,34 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
         for (int u = 0; u < NP; ++u) {
           const int key = KPI * u + p_key;
           const char* v = base + key * ROW + 32 * vchunk<DH>(p_at >> 1, key) + 16 * (p_at & 1);
-          dma16((has & seen(t0 + key)) ? v : reinterpret_cast<const char*>(zero_piece), to + 1024u * u);
+          dma16((v_has & seen(t0 + key)) ? v : reinterpret_cast<const char*>(zero_piece), to + 1024u * u);
         }
       }
     }
   };
   // 4 bits: the piece to LDS, as bf16 (head_dim 64: 32 lanes hold the 16 tokens, the others repeat them)
   auto store_k = [&](int j) {
-    const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+    const uint32_t w[4] = {k_piece.x, k_piece.y, k_piece.z, k_piece.w};
     char* at = lds + (j & 1) * BUF + (mine + p_key) * ROW;
     if (PPK == 4 || lane < 16 * PPK)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        *reinterpret_cast<uint4*>(at + 16 * kchunk<DH>(4 * p_at + x, mine + p_key)) = fp4_eight(w[x], fp4_scale(byte));
+        *reinterpret_cast<uint4*>(at + 16 * kchunk<DH>(4 * p_at + x, mine + p_key)) = fp4_eight(w[x], fp4_scale(k_byte));
   };
   auto store_v = [&](int j) {
-    const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+    const uint32_t w[4] = {v_piece.x, v_piece.y, v_piece.z, v_piece.w};
     char* at = lds + (2 + (j & 1)) * BUF + (mine + p_key) * ROW;
     if (PPK == 4 || lane < 16 * PPK)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         *reinterpret_cast<uint4*>(at + 32 * vchunk<DH>(2 * p_at + (x >> 1), mine + p_key) + 16 * (x & 1)) =
-            vis ? fp4_eight(w[x], fp4_scale(byte)) : make_uint4(0u, 0u, 0u, 0u);
+            vis ? fp4_eight(w[x], fp4_scale(v_byte)) : make_uint4(0u, 0u, 0u, 0u);
   };
-  // All of this wave's loads but the last NP are here, and every wave's are.
+  // Every wave's loads are here, and its reads of the block before done.
   auto meet = [&]() {
     if constexpr (FP4) __syncthreads();
-    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(NP) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
   };
-
-  // The halves of blocks (32 tokens) in which this wave has something to see, as
-  // positions in the run: ia .. ib - 1 (the few hidden ones between the first
-  // tokens and the window are run, masked).
-  int ia = 2 * j_end, ib = 2 * j_begin;
-  if (whi > max(wlo, 0)) {
-    const int shift = 2 * (blocks.sink - blocks.first), ft = a.window > 0 ? max(0, wlo - a.window + 1) : 0;
-    ia = a.window > 0 && blocks.token(j_begin, kKeys) < a.sinks ? 2 * j_begin : max(2 * j_begin, shift + ft / 32);
-    ib = min(2 * j_end, shift + (whi - 1) / 32 + 1);
-  }
 
   f32x16_t o[ND];  // O^T: rows 32 d + acc_row = values, column lr = the query
   float m, l;
@@ -595,61 +588,63 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           *reinterpret_cast<const bf16x8_t*>(K + lr * ROW + 16 * kchunk<DH>(2 * st + lh, lr)), qf[st], sc, 0, 0, 0);
   };
-  // Half i's scores masked where its tokens are not all seen, and the row's factor.
   auto visible = [&](int cur, uint32_t two, int k) {
     const int tok = cur + k;
     return static_cast<bool>(((two >> (k >> 4)) & 1u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
   };
-  auto statistics = [&](int i, f32x16_t& sc) {
-    const int cur = token_of(i);
-    const uint32_t two = (have >> (2 * (i & 1))) & 3u;
-    const bool whole = two == 3u && cur + 31 <= wlo && (a.window == 0 || whi - 1 - cur < a.window || cur + 32 <= a.sinks);
-    if (!whole) {
+  // Step i, between the scores of half i (formed in the step before) and its sums
+  // (formed in the next): half i's maximum; then, independent of each other, half
+  // i + 1's scores, half i's probabilities and the sums of half i - 1; then the
+  // rescaling, if the maximum has grown.  `two`, `two_before`: which 16-token tiles
+  // of half i, i - 1 have a page.
+  auto step = [&](int i, uint32_t two, uint32_t two_before, f32x16_t& sc, f32x16_t& next, bf16x8_t (&p)[2],
+                  const bf16x8_t (&before)[2], auto careful) {
+    {
+      const int cur = token_of(i);
+      const bool whole = two == 3u && i < 2 * j_end && cur + 31 <= wlo &&
+                         (a.window == 0 || whi - 1 - cur < a.window || cur + 32 <= a.sinks);
+      if (!whole) {
+        const uint32_t any = i < 2 * j_end ? two : 0u;  // (behind the last half: nothing)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = visible(cur, two, acc_row(r, lane)) ? sc[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) sc[r] = visible(cur, any, acc_row(r, lane)) ? sc[r] : -INFINITY;
+      }
     }
     float mx = sc[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
     mx = max_of_halves(mx) * c2;
     const bool grow = mx > m + kRescale;
-    if (__any(grow)) {
-      const float al = grow ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;  // (first block: 0)
-      if (grow) m = mx;
-      l *= al;
+    const float m_before = m;
+    if (grow) m = mx;
+
+    scores(i + 1, next);  // (behind the last half: unused)
+    float sum = 0.0f;
 #pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] *= al;
-    }
-  };
-  // O^T += V^T P^T of half i
-  auto gather = [&](int i, const f32x16_t& sc, auto careful) {
-    const char* V = lds + (2 + ((i >> 1) & 1)) * BUF + 32 * (i & 1) * ROW;
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
+        sum += e;
+        p[st][k] = static_cast<__bf16>(e);
+      }
+    const char* V = lds + (2 + (((i - 1) >> 1) & 1)) * BUF + 32 * ((i - 1) & 1) * ROW;
     auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
       const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
       const int c = 2 * d + ((lane >> 4) & 1);
       return join(tr_read(at + 32 * vchunk<DH>(c, tr_key)), tr_read(at + 8 * ROW + 32 * vchunk<DH>(c, tr_key + 8)));
     };
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      bf16x8_t pf;  // the probabilities of 16 keys
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
-        l += p;
-        pf[k] = static_cast<__bf16>(p);
-      }
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         bf16x8_t v = vfrag(st, d);
         if constexpr (careful.value) v = clean8(v);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf, o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, before[st], o[d], 0, 0, 0);
       }
-    }
     if constexpr (careful.value) {
-      const int cur = token_of(i);
-      const uint32_t two = (have >> (2 * (i & 1))) & 3u;
+      const int cur = token_of(i - 1);
       for (int k = 0; k < 32; ++k) {
-        const bool see = visible(cur, two, k);
+        const bool see = (i > 2 * j_begin) & visible(cur, two_before, k);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -660,21 +655,19 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
           }
       }
     }
-  };
-  // Step i forms half i + 1's scores beside half i's probabilities and sums, so that
-  // the matrix cores have work under the exponentials.  Keys of block j are read in
-  // steps 2 j - 1 and 2 j, its values in steps 2 j and 2 j + 1: an odd step brings
-  // the keys of the block after next, an even one the next block's values, each
-  // with two steps to arrive.
-  auto step = [&](int i, f32x16_t& sc, f32x16_t& next, auto careful) {
-    if (i >= ia && i < ib) {
-      statistics(i, sc);
-      scores(i + 1, next);  // (behind the wave's last half: unused)
-      gather(i, sc, careful);
-    } else if (i + 1 == ia) {
-      scores(i + 1, next);
+    // (the exponentials stay up here, beside the products, and do not sink below the branch)
+    asm volatile("" : "+v"(sum), "+v"(p[0]), "+v"(p[1]));
+    if (__any(grow)) {
+      const float al = grow ? __builtin_amdgcn_exp2f(m_before - m) : 1.0f;  // (first block: 0)
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= al;
     }
+    l += sum;
   };
+  // Keys of block j are read in steps 2 j - 1 and 2 j, its values in steps 2 j + 1
+  // and 2 j + 2: so one meeting a block, before an odd step, that brings the keys of
+  // the block after next and the values of the next.
   // A first run takes every value as finite; if a sum comes out infinite or NaN, a
   // second one keeps such values from the rows that do not see them (their zero
   // probability would not cancel them): the product runs on the finite values, and
@@ -686,34 +679,39 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     m = kLow;
     l = 0.0f;
+    // (before the first half: no scores, no probabilities)
     f32x16_t even, odd;
+    bf16x8_t p_even[2], p_odd[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd[r] = -INFINITY;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) p_even[st] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
     if (j_begin < j_end) {
       fill_pages(j_begin);
+      // (values of the block before the first: zeros, which that zero probability meets)
+#pragma unroll
+      for (int u = 0; u < BUF / 4096; ++u)
+        *reinterpret_cast<uint4*>(lds + (2 + ((j_begin - 1) & 1)) * BUF + 16 * (tid + 256 * u)) = make_uint4(0u, 0u, 0u, 0u);
       __syncthreads();
       find(j_begin);
       load_k(j_begin);
       if constexpr (FP4) store_k(j_begin);
-      load_v(j_begin);
-      if constexpr (FP4) store_v(j_begin);
       for (int j = j_begin - 1; j < j_end; ++j) {
-        if (j >= j_begin) {  // step 2 j
-          meet();
-          load_v(j + 1);  // (past the last block: the pool's first tokens, unused)
-          step(2 * j, even, odd, careful);
-          if constexpr (FP4) store_v(j + 1);
-        }
-        // step 2 j + 1
         meet();
         if (((j + 2 - j_begin) & 255) == 0) {
           fill_pages(j + 2);
           __syncthreads();
         }
-        const uint32_t h = k_have;  // of block j + 1
         find(j + 2);
-        load_k(j + 2);
-        step(2 * j + 1, odd, even, careful);
-        if constexpr (FP4) store_k(j + 2);
-        have = h;
+        load_k(j + 2);  // (past the last block: the pool's first tokens, unused)
+        load_v(j + 1);
+        // have: block j + 2's tiles in bits 0-3, j + 1's in 4-7, j's in 8-11
+        step(2 * j + 1, (have >> 10) & 3u, (have >> 8) & 3u, odd, even, p_odd, p_even, careful);
+        step(2 * j + 2, (have >> 4) & 3u, (have >> 10) & 3u, even, odd, p_even, p_odd, careful);
+        if constexpr (FP4) {
+          store_k(j + 2);
+          store_v(j + 1);
+        }
       }
     }
     float any = 0.0f;  // NaN once a sum is not finite
