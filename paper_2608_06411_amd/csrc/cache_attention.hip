@@ -573,6 +573,10 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
   };
 
+  // The step behind the last half of a block (32 tokens, counted from the first
+  // block of the run) that holds something for this wave: there is none after it.
+  const int last = whi > max(wlo, 0) ? min(2 * j_end, 2 * (blocks.sink - blocks.first) + (whi - 1) / 32 + 1) : -2;
+
   f32x16_t o[ND];  // O^T: rows 32 d + acc_row = values, column lr = the query
   float m, l;
   const float c2 = a.c2;
@@ -706,8 +710,10 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
         load_k(j + 2);  // (past the last block: the pool's first tokens, unused)
         load_v(j + 1);
         // have: block j + 2's tiles in bits 0-3, j + 1's in 4-7, j's in 8-11
-        step(2 * j + 1, (have >> 10) & 3u, (have >> 8) & 3u, odd, even, p_odd, p_even, careful);
-        step(2 * j + 2, (have >> 4) & 3u, (have >> 10) & 3u, even, odd, p_even, p_odd, careful);
+        if (2 * j + 1 <= last) {
+          step(2 * j + 1, (have >> 10) & 3u, (have >> 8) & 3u, odd, even, p_odd, p_even, careful);
+          step(2 * j + 2, (have >> 4) & 3u, (have >> 10) & 3u, even, odd, p_even, p_odd, careful);
+        }
         if constexpr (FP4) {
           store_k(j + 2);
           store_v(j + 1);
