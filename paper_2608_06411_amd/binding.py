@@ -168,7 +168,7 @@ def _need(t: torch.Tensor, name: str, shape, dtype, device):
     (device None: only checked to be a GPU device, by _on_gpu)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != tuple(shape) or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)}, got "
                          f"{t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
     if device is not None and t.device != device:
@@ -712,12 +712,13 @@ def _rows_ld(t, name: str, rows: int, heads: int, dh: int, dtype, device) -> int
     any multiple of 16 bytes apart, on a 16-byte boundary."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != dtype or t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != dh:
-        raise ValueError(f"{name}: expected {dtype} [at least {rows}, {heads}, {dh}], got {t.dtype} {tuple(t.shape)}")
+    shape = t.shape
+    if t.dtype != dtype or len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != dh:
+        raise ValueError(f"{name}: expected {dtype} [at least {rows}, {heads}, {dh}], got {t.dtype} {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
     row, head, one = t.stride()
-    if t.shape[0] <= 1:
+    if shape[0] <= 1:
         row = heads * dh
     if one != 1 or (heads > 1 and head != dh) or row < heads * dh or (row * t.element_size()) % 16 or t.data_ptr() % 16:
         raise ValueError(f"{name}: heads must be contiguous in a row, rows a multiple of 16 bytes apart and the first on a "
@@ -737,22 +738,20 @@ def _table(cache: KVCache, table, lens, B: int):
     return wide
 
 
-class _on:
-    """The device of a call's tensors as the current one while the library
-    launches on it (nothing to do when it is already)."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (current_stream makes an object: 2 us a call)
 
-    def __init__(self, device):
-        self.device = device
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-        return _stream(self.device)
-
-    def __exit__(self, *exc):
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.before)
+def _launch(where: str, fn, device, *args):
+    """fn(*args, stream) with the device of the call's tensors as the current one
+    and its current stream."""
+    i = device.index
+    if i == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(i) if _raw_stream else _stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _stream(device))
+    if status != MAP_OK:
+        raise MapError(status, where)
 
 
 def map_qk_norm_rope(rope: RopeParams, q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor,
@@ -764,36 +763,40 @@ def map_qk_norm_rope(rope: RopeParams, q: torch.Tensor, k: torch.Tensor, pos: to
     product); q_out and k_out may be q and k themselves.  Returns (q_out, k_out)."""
     R, Hq, dh = _dims(q, "q", 3)
     _, Hk, _ = _dims(k, "k", 3)
-    dt, dev = _dtype_code(q), q.device
+    dt, dev, dtype = _dtype_code(q), q.device, q.dtype
     if dh != rope.head_dim:
         raise ValueError(f"q: heads of {dh}, the rotation is for {rope.head_dim}")
     axes = len(rope.sections)
     if isinstance(pos, torch.Tensor) and pos.dim() == 1 and axes == 1:
         pos = pos[None]
-    if not isinstance(pos, torch.Tensor) or pos.dtype != torch.int32 or tuple(pos.shape) != (axes, R) or pos.device != dev \
-            or (R > 1 and pos.stride(1) != 1) or (axes > 1 and pos.stride(0) < R):
-        raise ValueError(f"pos: expected int32 [{axes}, {R}] on {dev}, its rows contiguous")
-    ldq = _rows_ld(q, "q", R, Hq, dh, q.dtype, dev)
-    ldk = _rows_ld(k, "k", R, Hk, dh, q.dtype, dev)
-    for name, g in (("q_norm", q_norm), ("k_norm", k_norm)):
+    if not isinstance(pos, torch.Tensor) or pos.dtype != torch.int32 or pos.shape != (axes, R) or pos.device != dev:
+        raise ValueError(f"pos: expected int32 [{axes}, {R}] on {dev}")
+    ldpos, one = pos.stride()
+    if axes == 1 or R == 0:
+        ldpos = R
+    if (one != 1 and R > 1) or ldpos < R:
+        raise ValueError(f"pos: its rows must be contiguous, got strides {pos.stride()}")
+    ldq = _rows_ld(q, "q", R, Hq, dh, dtype, dev)
+    ldk = _rows_ld(k, "k", R, Hk, dh, dtype, dev)
+    norms = [None, None]
+    for i, (name, g) in enumerate((("q_norm", q_norm), ("k_norm", k_norm))):
         if g is not None:
-            _need(g, name, (dh,), q.dtype, dev)
-            if g.data_ptr() % 16:
+            _need(g, name, (dh,), dtype, dev)
+            norms[i] = g.data_ptr()
+            if norms[i] % 16:
                 raise ValueError(f"{name}: not on a 16-byte boundary")
     if q_out is None:
-        q_out = torch.empty(R, Hq, dh, dtype=q.dtype, device=dev)
+        q_out, ldqo = torch.empty_like(q, memory_format=torch.contiguous_format), Hq * dh
+    else:
+        ldqo = _rows_ld(q_out, "q_out", R, Hq, dh, dtype, dev)
     if k_out is None:
-        k_out = torch.empty(R, Hk, dh, dtype=q.dtype, device=dev)
-    ldqo = _rows_ld(q_out, "q_out", R, Hq, dh, q.dtype, dev)
-    ldko = _rows_ld(k_out, "k_out", R, Hk, dh, q.dtype, dev)
+        k_out, ldko = torch.empty_like(k, memory_format=torch.contiguous_format), Hk * dh
+    else:
+        ldko = _rows_ld(k_out, "k_out", R, Hk, dh, dtype, dev)
     _on_gpu(q, "q")
-    if R == 0:
-        return q_out, k_out
-    with _on(dev) as stream:
-        _check(lib().map_qk_norm_rope(rope._ref, dt, R, Hq, Hk, q.data_ptr(), ldq, k.data_ptr(), ldk, pos.data_ptr(),
-                                      max(R, pos.stride(0) if axes > 1 else R), None if q_norm is None else q_norm.data_ptr(),
-                                      None if k_norm is None else k_norm.data_ptr(), q_out.data_ptr(), ldqo,
-                                      k_out.data_ptr(), ldko, stream), "map_qk_norm_rope")
+    if R > 0:
+        _launch("map_qk_norm_rope", lib().map_qk_norm_rope, dev, rope._ref, dt, R, Hq, Hk, q.data_ptr(), ldq, k.data_ptr(), ldk,
+                pos.data_ptr(), ldpos, norms[0], norms[1], q_out.data_ptr(), ldqo, k_out.data_ptr(), ldko)
     return q_out, k_out
 
 
@@ -809,9 +812,8 @@ def map_cache_append(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, k:
     _on_gpu(k, "k")
     if off.rows == 0:
         return
-    with _on(cache.device) as stream:
-        _check(lib().map_cache_append(cache._ref, MAP_BF16, off.B, table.data_ptr(), wide, lens.data_ptr(), k.data_ptr(), ldk,
-                                      v.data_ptr(), ldv, off._arr, stream), "map_cache_append")
+    _launch("map_cache_append", lib().map_cache_append, cache.device, cache._ref, MAP_BF16, off.B, table.data_ptr(), wide,
+            lens.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, off._arr)
 
 
 def map_cache_read(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, seq_off, slots: Optional[torch.Tensor] = None,
@@ -822,21 +824,19 @@ def map_cache_read(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, seq_
     off = _seq(seq_off)
     wide = _table(cache, table, lens, off.B)
     shape = (off.rows, cache.n_kv_heads, cache.head_dim)
+    if slots is not None:
+        _need(slots, "slots", (off.rows,), torch.int32, cache.device)
+    ld = shape[1] * shape[2]
+    ldk = ld if k_out is None else _rows_ld(k_out, "k_out", *shape, torch.bfloat16, cache.device)
+    ldv = ld if v_out is None else _rows_ld(v_out, "v_out", *shape, torch.bfloat16, cache.device)
+    _on_gpu(cache.k, "cache")
     if k_out is None:
         k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
     if v_out is None:
         v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    ldk = _rows_ld(k_out, "k_out", *shape, torch.bfloat16, cache.device)
-    ldv = _rows_ld(v_out, "v_out", *shape, torch.bfloat16, cache.device)
-    if slots is not None:
-        _need(slots, "slots", (off.rows,), torch.int32, cache.device)
-    _on_gpu(k_out, "k_out")
-    if off.rows == 0:
-        return k_out, v_out
-    with _on(cache.device) as stream:
-        _check(lib().map_cache_read(cache._ref, MAP_BF16, off.B, table.data_ptr(), wide, lens.data_ptr(),
-                                    None if slots is None else slots.data_ptr(), off._arr, k_out.data_ptr(), ldk,
-                                    v_out.data_ptr(), ldv, stream), "map_cache_read")
+    if off.rows > 0:
+        _launch("map_cache_read", lib().map_cache_read, cache.device, cache._ref, MAP_BF16, off.B, table.data_ptr(), wide,
+                lens.data_ptr(), None if slots is None else slots.data_ptr(), off._arr, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv)
     return k_out, v_out
 
 
@@ -861,23 +861,21 @@ def map_cache_attention(cache: KVCache, table: torch.Tensor, lens: torch.Tensor,
     wide = _table(cache, table, lens, off.B)
     rows, heads, dh = _dims(q, "q", 3)
     ldq = _rows_ld(q, "q", off.rows, heads, cache.head_dim, torch.bfloat16, cache.device)
-    if out is None:
-        out = torch.empty(rows, heads, dh, dtype=torch.bfloat16, device=cache.device)
-    ldo = _rows_ld(out, "out", off.rows, heads, dh, torch.bfloat16, cache.device)
+    ldo = heads * dh if out is None else _rows_ld(out, "out", off.rows, heads, dh, torch.bfloat16, cache.device)
     if heads % cache.n_kv_heads or not 1 <= heads <= 1024:
         raise ValueError(f"q: {heads} heads over {cache.n_kv_heads} key/value heads")
     if window < 0 or sinks < 0:
         raise ValueError("window and sinks must not be negative")
     _on_gpu(q, "q")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if off.rows == 0:
         return out
     ws = cache_attention_workspace(cache, off, heads, table) if workspace is None else workspace
     _need_ws(ws, 256, cache.device)
-    with _on(cache.device) as stream:
-        _check(lib().map_cache_attention(cache._ref, MAP_BF16, off.B, heads, table.data_ptr(), wide, lens.data_ptr(),
-                                         q.data_ptr(), ldq, off._arr, dh ** -0.5 if scale is None else float(scale),
-                                         int(window), int(sinks), out.data_ptr(), ldo, ws.data_ptr(), ws.numel(), stream),
-               "map_cache_attention")
+    _launch("map_cache_attention", lib().map_cache_attention, cache.device, cache._ref, MAP_BF16, off.B, heads, table.data_ptr(),
+            wide, lens.data_ptr(), q.data_ptr(), ldq, off._arr, dh ** -0.5 if scale is None else float(scale), int(window),
+            int(sinks), out.data_ptr(), ldo, ws.data_ptr(), ws.numel())
     return out
 
 

@@ -87,7 +87,7 @@ __device__ __forceinline__ Blocks visible_blocks(int lo, int hi, int window, int
 constexpr int kStepWaves = 4;
 
 template <int DH, bool FP4> struct StepShape {
-  static constexpr int KB = 32, NT = KB / 16, NM = KB / 32, ND = DH / 16, NS = DH / 32;
+  static constexpr int KB = FP4 || DH == 64 ? 64 : 32, NT = KB / 16, NM = KB / 32, ND = DH / 16, NS = DH / 32;
   static constexpr int VROW = 2 * DH;                       // bytes of a token's values in LDS
   static constexpr int VPIECE = FP4 ? DH / 2 : 2 * DH;      // and in a page
   static constexpr int NV = KB * VPIECE / 1024;             // 16-byte pieces a lane
@@ -116,8 +116,8 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
   const int i_lo = col0 / a.G, i_hi = min(col0 + 15, cols - 1) / a.G;
   const int lo = base + i_lo, hi = base + i_hi + 1;
   const Blocks blocks = visible_blocks(lo, hi, a.window, a.sinks, KB);
-  const int part = blockIdx.x, j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.splits);
-  const int j0 = static_cast<int>((long long)blocks.count * part / a.splits) + wave;
+  const int part = blockIdx.x, j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.step_splits);
+  const int j0 = static_cast<int>((long long)blocks.count * part / a.step_splits) + wave;
 
   // this lane's query
   const int col = min(col0 + lc, cols - 1), row = col / a.G, head = kvh * a.G + col - row * a.G, me = base + row;
@@ -173,9 +173,11 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
     }
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      constexpr int PPK = X::VPIECE / 16;  // pieces a key
-      const int e = u * 64 + lane, key = e / PPK, c = e % PPK;
-      const long long r = (NT == 1 || key < 16 ? rows[0] : rows[NT - 1]) + (key & 15);
+      constexpr int PPK = X::VPIECE / 16, KPU = 64 / PPK;  // pieces a key, keys a load
+      const int key = u * KPU + lane / PPK, c = lane % PPK;
+      long long r = rows[u * KPU / 16];
+      if (KPU == 32 && lane >= 32) r = rows[u * KPU / 16 + 1];
+      r += key & 15;
       vr[u] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.c.v) + r * X::VPIECE + 16 * c);
       if constexpr (FP4) vsb[u] = a.c.vs[r * NS + c];
     }
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       constexpr int PPK = X::VPIECE / 16;
-      const int e = u * 64 + lane, key = e / PPK, c = e % PPK, tok = cur + key;
+      const int key = u * (64 / PPK) + lane / PPK, c = lane % PPK, tok = cur + key;
       const bool see = whole | (((held >> (key >> 4)) & 1u) & (tok < hi) & ((tok >= from_lo) | (tok < a.sinks)));
       if constexpr (FP4) {
 #pragma unroll
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
     for (int k = 0; k < PER; ++k) v[k] = fmaf(f, src[k], v[k]);
   }
   const int rr = (col0 + c) / a.G, hh = kvh * a.G + col0 + c - rr * a.G;
-  if (a.splits == 1) {
+  if (a.step_splits == 1) {
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     bf16_t* out = static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0;
     union { uint2 u[PER / 4]; bf16_t e[PER]; } w;
@@ -386,12 +388,17 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) 
   const long long item = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH, items = (long long)a.off[a.B] * a.Hq;
   if (item >= items) return;
   const int r = static_cast<int>(item / a.Hq), h = static_cast<int>(item - (long long)r * a.Hq), d0 = 4 * (threadIdx.x % LPH);
+  int b = 0;  // the row's sequence: the last that starts at or before it
+  for (int s = MAP_CACHE_MAX_BATCH / 2; s > 0; s >>= 1)
+    if (b + s < a.B && a.off[b + s] <= r) b += s;
+  const int splits = a.off[b + 1] - a.off[b] <= a.step_rows ? a.step_splits : a.prompt_splits;
+  if (splits == 1) return;  // (written by its own kernel)
   float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < a.splits; ++s) {
+  for (int s = 0; s < splits; ++s) {
     const float2 ml = a.part_ml[(long long)s * items + item];
     if (ml.y != 0.0f) mm = fmaxf(mm, ml.x);
   }
-  for (int s = 0; s < a.splits; ++s) {
+  for (int s = 0; s < splits; ++s) {
     const float2 ml = a.part_ml[(long long)s * items + item];
     if (ml.y == 0.0f) continue;
     const float f = __builtin_amdgcn_exp2f(ml.x - mm);
@@ -451,8 +458,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   __shared__ __attribute__((aligned(1024))) char lds[4 * BUF];  // K, K, V, V
   __shared__ int4 pages[256];
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
-  const int tiles = gridDim.y / a.splits, part = blockIdx.y % a.splits;
-  const int q0 = (tiles - 1 - static_cast<int>(blockIdx.y) / a.splits) * 32 * NW;  // the longest first
+  const int tiles = gridDim.y / a.prompt_splits, part = blockIdx.y % a.prompt_splits;
+  const int q0 = (tiles - 1 - static_cast<int>(blockIdx.y) / a.prompt_splits) * 32 * NW;  // the longest first
   if (n <= a.step_rows || q0 >= n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5, h = blockIdx.x, kvh = h / a.G;
@@ -462,8 +469,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   const int me = wlo + lr, from = a.window > 0 ? me - a.window + 1 : 0;  // this lane's, and its window's first
   const int from_lo = a.window > 0 ? lo - a.window + 1 : 0;
   const Blocks blocks = visible_blocks(lo, hi, a.window, a.sinks, kKeys);
-  const int j_begin = static_cast<int>((long long)blocks.count * part / a.splits);
-  const int j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.splits);
+  const int j_begin = static_cast<int>((long long)blocks.count * part / a.prompt_splits);
+  const int j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.prompt_splits);
 
   bf16x8_t qf[NS];  // the query's values 16 st + 8 lh + (0..7)
   {
@@ -732,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   if (whi <= wlo) return;
   l += __shfl_xor(l, 32, 64);
   const int i = q0 + 32 * wave + lr;  // this lane's row
-  if (a.splits > 1) {
+  if (a.prompt_splits > 1) {
     if (i >= n) return;
     const long long at = ((long long)part * a.off[a.B] + r0 + i) * a.Hq + h;
     if (lh == 0) a.part_ml[at] = make_float2(m, l);
@@ -774,49 +781,51 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 constexpr int kStepRows = 16;
 
 struct Plan {
-  int step_most, prompt_most;  // the longest of each kind (0: none)
-  int tiles;                   // 16-column tiles of the longest few-row sequence
-  int splits;
+  int step_most, prompt_most;      // the longest sequence of each kind (0: none)
+  int tiles;                       // 16-column tiles of the longest few-row sequence
+  int step_splits, prompt_splits;  // parts of the tokens
 };
 
-}  // namespace
-
-namespace {
 Plan make_plan(const int* off, int B, int Hq, int Hkv, long long tokens, int cus) {
-  Plan p{0, 0, 1, 1};
+  Plan p{0, 0, 1, 1, 1};
   const int G = Hq / Hkv;
-  long long groups = 0;
+  long long step_groups = 0, prompt_groups = 0;
   for (int b = 0; b < B; ++b) {
     const int n = off[b + 1] - off[b];
+    if (n == 0) continue;
     if (n <= kStepRows) {
       p.step_most = max(p.step_most, n);
-      groups += (long long)((n * G + 15) / 16) * Hkv;
+      step_groups += (long long)((n * G + 15) / 16) * Hkv;
     } else {
       p.prompt_most = max(p.prompt_most, n);
-      groups += (long long)((n + 127) / 128) * Hq;
+      prompt_groups += (long long)((n + 127) / 128) * Hq;
     }
   }
   p.tiles = max(1, (p.step_most * G + 15) / 16);
-  const long long want = 2LL * cus;
-  const long long s = min(min(want / max(groups, 1LL), tokens / 256), 64LL);
-  p.splits = static_cast<int>(max(s, 1LL));
+  auto parts = [&](long long groups, long long want, long long least) {
+    return groups == 0 ? 1 : static_cast<int>(max(1LL, min(min(want / groups, tokens / least), 64LL)));
+  };
+  p.step_splits = parts(step_groups, 2LL * cus, 256);
+  p.prompt_splits = parts(prompt_groups, 2LL * cus, 512);
   return p;
 }
+
 }  // namespace
 
-// The parts a call is split into, for the workspace (0 floats: none).
 int cache_attention_splits(const int* off, int B, int Hq, int Hkv, long long max_tokens, int cus) {
-  return make_plan(off, B, Hq, Hkv, max_tokens, cus).splits;
+  const Plan p = make_plan(off, B, Hq, Hkv, max_tokens, cus);
+  return max(p.step_splits, p.prompt_splits);
 }
 
 hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cus, hipStream_t s) {
   const Plan p = make_plan(a.off, a.B, a.Hq, a.Hq / a.G, max_tokens, cus);
-  a.splits = p.splits;
+  a.step_splits = p.step_splits;
+  a.prompt_splits = p.prompt_splits;
   a.tiles = p.tiles;
   a.step_rows = kStepRows;
   hipError_t e = hipSuccess;
   if (p.step_most > 0) {
-    const dim3 grid(p.splits, a.Hq / a.G * p.tiles, a.B), block(64 * kStepWaves);
+    const dim3 grid(p.step_splits, a.Hq / a.G * p.tiles, a.B), block(64 * kStepWaves);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, true>, grid, block, 0, s, a);
@@ -825,7 +834,7 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cu
                       : launch_kernel("cache_step", cache_step_kernel<64, false>, grid, block, 0, s, a);
   }
   if (e == hipSuccess && p.prompt_most > 0) {
-    const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.splits, a.B), block(256);
+    const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.prompt_splits, a.B), block(256);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, true>, grid, block, 0, s, a);
@@ -833,7 +842,7 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cu
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, false>, grid, block, 0, s, a);
   }
-  if (e == hipSuccess && p.splits > 1) {
+  if (e == hipSuccess && max(p.step_splits, p.prompt_splits) > 1) {
     const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
     const dim3 grid(static_cast<unsigned>((items + per - 1) / per)), block(256);
     e = a.Dh == 128 ? launch_kernel("cache_join", cache_join_kernel<128>, grid, block, 0, s, a)

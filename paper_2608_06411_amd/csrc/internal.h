@@ -60,6 +60,7 @@ hipError_t launch_kernel(const char* name, void (*kernel)(P...), dim3 grid, dim3
   void* argv[sizeof...(P)];
   kernel_argv(argv, vals, std::index_sequence_for<P...>{});
   const LaunchEvents ev = timing_events(name);
+  if (!ev.start) return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, lds_bytes, s);
   return hipExtLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, lds_bytes, s, ev.start,
                             ev.stop, 0);
 }
@@ -474,11 +475,11 @@ struct CacheAttnArgs {
   int B, Hq, G, Dh, window, sinks;
   float c2;               // scale log2(e)
   bool fp4;
-  // set by the launch: parts of the tokens, 16-column tiles of a few-row sequence,
-  // the most rows of one
-  int splits, tiles, step_rows;
-  float* part_o;          // [splits][rows][Hq][Dh] each part's sums, when splits > 1
-  float2* part_ml;        // [splits][rows][Hq] and (m, l)
+  // set by the launch: 16-column tiles of the longest few-row sequence, the most rows
+  // of one, parts of the tokens of both kinds of sequences
+  int tiles, step_rows, step_splits, prompt_splits;
+  float* part_o;          // [part][rows][Hq][Dh] each part's sums, where there are several
+  float2* part_ml;        // [part][rows][Hq] and (m, l)
   int off[MAP_CACHE_MAX_BATCH + 1];
 };
 // Parts that a call is split into (the workspace holds their sums), and the call.
