@@ -59,6 +59,16 @@ __device__ __forceinline__ bf16x8_t clean8(bf16x8_t v) {
   return __builtin_bit_cast(bf16x8_t, make_uint4(word_clean(u.x), word_clean(u.y), word_clean(u.z), word_clean(u.w)));
 }
 
+// N values over their sum, as bf16; zeros where nothing was summed.
+template <int N> __device__ __forceinline__ void write_row(bf16_t* out, const float* v, float sum) {
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  union { uint2 u[N / 4]; bf16_t e[N]; } w;
+#pragma unroll
+  for (int k = 0; k < N; ++k) w.e[k] = f32_to_bf16(v[k] * inv);
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k) reinterpret_cast<uint2*>(out)[k] = w.u[k];
+}
+
 // The blocks of KB tokens that rows lo .. hi - 1 (token indices) see any of:
 // those of the first tokens, then those from the first row's window to the last row.
 struct Blocks {
@@ -76,14 +86,17 @@ __device__ __forceinline__ Blocks visible_blocks(int lo, int hi, int window, int
 }
 
 // ---------------------------------------------------------------- few rows
-// Single tokens and a few rows behind a cache.  A workgroup takes 16 columns, the
-// (row, query head) pairs of one key/value head, and one of S parts of the tokens;
-// each of its four waves streams every fourth block of that part on its own (no
-// barrier until the end) and they join.  Bound: the cache's bytes.  A block's
-// keys and values are loaded a block ahead, straight to registers (16 bytes a
-// lane: keys as the first product's operand, values on their way to LDS), so that
-// each wave always has a block in flight; the matrix products and the
-// softmax (a few hundred clocks a block) hide behind them.
+// Single tokens and a few rows behind a cache.  The work is one run of blocks: of
+// every sequence, key/value head and tile of 16 columns (the (row, query head)
+// pairs of that head), the tokens the tile sees.  Each workgroup takes an equal
+// stretch of that run, whatever the sequences' lengths; a tile whose blocks lie in
+// several stretches leaves its sums for the kernel after it to join.  Within a
+// stretch each of the four waves streams every fourth block on its own (no
+// barrier until a tile's end).  Bound: the cache's bytes.  A block's keys and
+// values are loaded a block ahead, straight to registers (16 bytes a lane: keys as
+// the first product's operand, values on their way to LDS), so that each wave
+// always has a block in flight; the matrix products and the softmax (a few hundred
+// clocks a block) hide behind them.
 constexpr int kStepWaves = 4;
 
 template <int DH, bool FP4> struct StepShape {
@@ -95,11 +108,58 @@ template <int DH, bool FP4> struct StepShape {
   static constexpr int BYTES = kStepWaves * (KB * VROW > 16 * OLD * 4 ? KB * VROW : 16 * OLD * 4);
 };
 
-// Position of 32-byte chunk c of key k's row of V in LDS: the 32 lanes of half a
-// transposing read (8 keys' one chunk, or 4 keys' two) name all 64 banks once.
+// Position of 32-byte chunk c of key k's row of V in LDS.  The 32 lanes of half a
+// transposing read (8 keys' one chunk, or 4 keys' two) name all 64 banks once, and
+// so do 8 lanes that write widened 4-bit values (2 keys' every other chunk).
 template <int DH> __device__ __forceinline__ int vchunk(int c, int k) {
-  return DH == 128 ? c ^ (((k & 3) << 1) | ((k >> 2) & 1)) : c ^ ((k & 2) | ((k >> 2) & 1));
+  return DH == 128 ? c ^ (((k & 3) << 1) | ((k ^ (k >> 2)) & 1)) : c ^ ((k & 2) | (((k >> 1) ^ (k >> 2)) & 1));
 }
+
+// The blocks that column tile ct of a sequence of n rows and len tokens sees.
+__device__ __forceinline__ Blocks tile_blocks(const CacheAttnArgs& a, int n, int len, int ct, int kb) {
+  const int lo = len - n + 16 * ct / a.G, hi = len - n + min(16 * ct + 15, n * a.G - 1) / a.G + 1;
+  return visible_blocks(lo, hi, a.window, a.sinks, kb);
+}
+
+// Where each sequence's blocks begin in the run, from the lengths on the device
+// (256 threads, one sequence each).
+struct StepRun {
+  int begin[MAP_CACHE_MAX_BATCH + 1];  // [B]: all blocks
+  int wave_sum[4];
+  int len[MAP_CACHE_MAX_BATCH], found;
+};
+__device__ __forceinline__ void lay_out_run(const CacheAttnArgs& a, StepRun& run, int kb) {
+  const int t = threadIdx.x, lane = t & 63;
+  int v = 0;
+  if (t < a.B) {
+    const int n = a.off[t + 1] - a.off[t], len = cache_len(a.c, t);
+    run.len[t] = len;
+    if (n > 0 && n <= a.step_rows)
+      for (int ct = 0; 16 * ct < n * a.G; ++ct) v += tile_blocks(a, n, len, ct, kb).count;
+    v *= a.c.heads;
+  }
+  int before = v;  // this sequence's and those before it in the wave
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(before, o, 64);
+    if (lane >= o) before += u;
+  }
+  if (lane == 63) run.wave_sum[t >> 6] = before;
+  __syncthreads();
+  for (int w = 0; w < (t >> 6); ++w) before += run.wave_sum[w];
+  if (t < a.B) run.begin[t + 1] = before;
+  if (t == 0) run.begin[0] = 0;
+  __syncthreads();
+}
+// Equal stretches: the first total % groups are one block longer.
+struct Stretches {
+  int each, more;
+  __device__ __forceinline__ Stretches(int total, int groups) : each(total / groups), more(total % groups) {}
+  __device__ __forceinline__ int begin(int w) const { return each * w + min(w, more); }
+  __device__ __forceinline__ int of(int x) const {  // the stretch that block x lies in
+    return x < more * (each + 1) ? x / (each + 1) : more + (x - more * (each + 1)) / each;
+  }
+};
 
 template <int DH, bool FP4>
 __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const CacheAttnArgs a) {
@@ -107,17 +167,47 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
   constexpr int KB = X::KB, NT = X::NT, NM = X::NM, ND = X::ND, NS = X::NS, NV = X::NV;
   __shared__ __attribute__((aligned(1024))) char lds[X::BYTES];
   __shared__ float ms[kStepWaves][16], ls[kStepWaves][16];
-  const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
-  const int kvh = blockIdx.y / a.tiles, col0 = (blockIdx.y - kvh * a.tiles) * 16, cols = n * a.G;
-  if (n > a.step_rows || col0 >= cols) return;
+  __shared__ StepRun run_of;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lc = lane & 15, g4 = lane >> 4;
-  const int len = cache_len(a.c, b), base = len - n;  // token of the sequence's first new row
+  const bool stretch = a.groups > 0;  // otherwise a workgroup has one tile, and all of it
+  int b = blockIdx.z;
+  int x = 0, x_begin = 0, x_end = 0;
+  if (stretch) {
+    lay_out_run(a, run_of, KB);
+    const Stretches all(__builtin_amdgcn_readfirstlane(run_of.begin[a.B]), a.groups);
+    x = x_begin = all.begin(blockIdx.x);
+    x_end = all.begin(blockIdx.x + 1);
+    if (x >= x_end) return;
+    if (tid < a.B && run_of.begin[tid] <= x && x < run_of.begin[tid + 1]) run_of.found = tid;
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(run_of.found);
+  }
+  for (;;) {
+  const int r0 = a.off[b], n = a.off[b + 1] - r0, cols = n * a.G;
+  const int len = stretch ? __builtin_amdgcn_readfirstlane(run_of.len[b]) : cache_len(a.c, b);
+  int kvh, ct, p0 = 0;
+  if (stretch) {
+    const int first = __builtin_amdgcn_readfirstlane(run_of.begin[b]), after = __builtin_amdgcn_readfirstlane(run_of.begin[b + 1]);
+    const int per_head = (after - first) / a.c.heads;
+    kvh = (x - first) / per_head;
+    p0 = x - first - kvh * per_head;
+    for (ct = 0;; ++ct) {
+      const int count = tile_blocks(a, n, len, ct, KB).count;
+      if (p0 < count) break;
+      p0 -= count;
+    }
+  } else {
+    kvh = blockIdx.x / a.tiles;
+    ct = blockIdx.x - kvh * a.tiles;
+    if (n > a.step_rows || 16 * ct >= cols) return;
+  }
+  const int col0 = 16 * ct, base = len - n;  // base: token of the sequence's first new row
   const int i_lo = col0 / a.G, i_hi = min(col0 + 15, cols - 1) / a.G;
   const int lo = base + i_lo, hi = base + i_hi + 1;
   const Blocks blocks = visible_blocks(lo, hi, a.window, a.sinks, KB);
-  const int part = blockIdx.x, j_end = static_cast<int>((long long)blocks.count * (part + 1) / a.step_splits);
-  const int j0 = static_cast<int>((long long)blocks.count * part / a.step_splits) + wave;
+  const int j_end = stretch ? min(blocks.count, p0 + x_end - x) : blocks.count;
+  const int j0 = p0 + wave;
 
   // this lane's query
   const int col = min(col0 + lc, cols - 1), row = col / a.G, head = kvh * a.G + col - row * a.G, me = base + row;
@@ -236,19 +326,21 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
     for (int u = 0; u < NV; ++u) {
       constexpr int PPK = X::VPIECE / 16;
       const int key = u * (64 / PPK) + lane / PPK, c = lane % PPK, tok = cur + key;
-      const bool see = whole | (((held >> (key >> 4)) & 1u) & (tok < hi) & ((tok >= from_lo) | (tok < a.sinks)));
+      if (!whole) {
+        if (!(((held >> (key >> 4)) & 1u) & (tok < hi) & ((tok >= from_lo) | (tok < a.sinks)))) {
+          vr[u] = make_uint4(0u, 0u, 0u, 0u);
+          vsb[u] = 0u;  // (4 bits: zero codes need a scale that is no NaN)
+        }
+      }
       if constexpr (FP4) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const uint32_t w = x == 0 ? vr[u].x : x == 1 ? vr[u].y : x == 2 ? vr[u].z : vr[u].w;
-          uint4 v = fp4_eight(w, fp4_scale(vsb[u]));
-          if (!see) v = make_uint4(0u, 0u, 0u, 0u);
-          *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) = v;
+          *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(2 * c + (x >> 1), key) + 16 * (x & 1)) =
+              fp4_eight(w, fp4_scale(vsb[u]));
         }
       } else {
-        uint4 v = vr[u];
-        if (!see) v = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(c >> 1, key) + 16 * (c & 1)) = v;
+        *reinterpret_cast<uint4*>(vt + key * X::VROW + 32 * vchunk<DH>(c >> 1, key) + 16 * (c & 1)) = vr[u];
       }
     }
     // the next block's loads under the rest of this one
@@ -348,42 +440,92 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
   __syncthreads();
   constexpr int PER = DH / 16;  // values a thread
   const int c = tid >> 4, d0 = (tid & 15) * PER;
-  if (col0 + c >= cols) return;
-  float mm = kLow, sum = 0.0f, v[PER];
+  if (col0 + c < cols) {
+    float mm = kLow, sum = 0.0f, v[PER];
 #pragma unroll
-  for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, ms[w][c]);
+    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, ms[w][c]);
 #pragma unroll
-  for (int k = 0; k < PER; ++k) v[k] = 0.0f;
+    for (int k = 0; k < PER; ++k) v[k] = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kStepWaves; ++w) {
-    const float lw = ls[w][c], f = lw == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ms[w][c] - mm);
-    if (lw == 0.0f) continue;
-    sum = fmaf(f, lw, sum);
-    const float* src = reinterpret_cast<const float*>(lds) + (w * 16 + c) * X::OLD + d0;
+    for (int w = 0; w < kStepWaves; ++w) {
+      const float lw = ls[w][c], f = __builtin_amdgcn_exp2f(ms[w][c] - mm);
+      if (lw == 0.0f) continue;
+      sum = fmaf(f, lw, sum);
+      const float* src = reinterpret_cast<const float*>(lds) + (w * 16 + c) * X::OLD + d0;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) v[k] = fmaf(f, src[k], v[k]);
+      for (int k = 0; k < PER; ++k) v[k] = fmaf(f, src[k], v[k]);
+    }
+    if (p0 == 0 && j_end == blocks.count) {
+      const int rr = (col0 + c) / a.G, hh = kvh * a.G + col0 + c - rr * a.G;
+      write_row<PER>(static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0, v, sum);
+    } else {  // the stretch's first tile, or its last
+      const long long at = (2LL * blockIdx.x + (x == x_begin ? 0 : 1)) * 16 + c;
+      if (d0 == 0) a.step_ml[at] = make_float2(mm, sum);
+      float4* po = reinterpret_cast<float4*>(a.step_o + at * DH + d0);
+#pragma unroll
+      for (int k = 0; k < PER / 4; ++k) po[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    }
   }
-  const int rr = (col0 + c) / a.G, hh = kvh * a.G + col0 + c - rr * a.G;
-  if (a.step_splits == 1) {
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    bf16_t* out = static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0;
-    union { uint2 u[PER / 4]; bf16_t e[PER]; } w;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) w.e[k] = f32_to_bf16(v[k] * inv);
-#pragma unroll
-    for (int k = 0; k < PER / 4; ++k) reinterpret_cast<uint2*>(out)[k] = w.u[k];
-  } else {
-    const long long at = ((long long)part * a.off[a.B] + r0 + rr) * a.Hq + hh;
-    if (d0 == 0) a.part_ml[at] = make_float2(mm, sum);
-    float4* po = reinterpret_cast<float4*>(a.part_o + at * DH + d0);
-#pragma unroll
-    for (int k = 0; k < PER / 4; ++k) po[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+  if (!stretch) return;
+  x += j_end - p0;
+  if (x >= x_end) return;
+  __syncthreads();  // (LDS is read out)
+  while (x >= __builtin_amdgcn_readfirstlane(run_of.begin[b + 1])) ++b;
   }
 }
 
-// Joins the parts: out = sum_s f_s o_s / sum_s f_s l_s, f_s = 2^(m_s - max m).
+// The tiles that lie in several stretches: out = sum_s f_s o_s / sum_s f_s l_s over
+// their pieces s, f_s = 2^(m_s - max m).  A tile that sees nothing is in none: zeros.
+template <int DH, bool FP4>
+__global__ __launch_bounds__(256) void cache_step_join_kernel(const CacheAttnArgs a) {
+  constexpr int KB = StepShape<DH, FP4>::KB, PER = DH / 16;
+  __shared__ StepRun run_of;
+  const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0, cols = n * a.G;
+  const int kvh = blockIdx.x / a.tiles, ct = blockIdx.x - kvh * a.tiles;
+  if (n > a.step_rows || 16 * ct >= cols) return;
+  lay_out_run(a, run_of, KB);
+  const int len = run_of.len[b];
+  int first = run_of.begin[b] + kvh * ((run_of.begin[b + 1] - run_of.begin[b]) / a.c.heads);
+  for (int t = 0; t < ct; ++t) first += tile_blocks(a, n, len, t, KB).count;
+  const int last = first + tile_blocks(a, n, len, ct, KB).count - 1;
+  const Stretches all(run_of.begin[a.B], a.groups);
+  int w0 = 0, w1 = -1;  // the stretches it lies in
+  if (last >= first) {
+    w0 = __builtin_amdgcn_readfirstlane(all.of(first));
+    w1 = __builtin_amdgcn_readfirstlane(all.of(last));
+    if (w0 == w1) return;  // (written whole)
+  }
+  const int c = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * PER;
+  if (16 * ct + c >= cols) return;
+  float mm = kLow, sum = 0.0f, v[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) v[k] = 0.0f;
+  auto piece = [&](int w) {  // the first tile of its stretch, or the last
+    return (2LL * w + (first <= all.begin(w) ? 0 : 1)) * 16 + c;
+  };
+  for (int w = w0; w <= w1; ++w) mm = fmaxf(mm, a.step_ml[piece(w)].x);
+#pragma unroll 4
+  for (int w = w0; w <= w1; ++w) {
+    const float2 ml = a.step_ml[piece(w)];
+    const float f = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mm);
+    const float4* po = reinterpret_cast<const float4*>(a.step_o + piece(w) * DH + d0);
+    sum = fmaf(f, ml.y, sum);
+#pragma unroll
+    for (int k = 0; k < PER / 4; ++k) {
+      const float4 o = po[k];
+      v[4 * k] = fmaf(f, o.x, v[4 * k]);
+      v[4 * k + 1] = fmaf(f, o.y, v[4 * k + 1]);
+      v[4 * k + 2] = fmaf(f, o.z, v[4 * k + 2]);
+      v[4 * k + 3] = fmaf(f, o.w, v[4 * k + 3]);
+    }
+  }
+  const int rr = (16 * ct + c) / a.G, hh = kvh * a.G + 16 * ct + c - rr * a.G;
+  write_row<PER>(static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0, v, sum);
+}
+
+// Joins the parts of the prompts' rows in the same way.
 template <int DH>
-__global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheAttnArgs a) {
   constexpr int LPH = DH / 4;  // lanes a row and head
   const long long item = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH, items = (long long)a.off[a.B] * a.Hq;
   if (item >= items) return;
@@ -391,14 +533,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) 
   int b = 0;  // the row's sequence: the last that starts at or before it
   for (int s = MAP_CACHE_MAX_BATCH / 2; s > 0; s >>= 1)
     if (b + s < a.B && a.off[b + s] <= r) b += s;
-  const int splits = a.off[b + 1] - a.off[b] <= a.step_rows ? a.step_splits : a.prompt_splits;
-  if (splits == 1) return;  // (written by its own kernel)
+  if (a.off[b + 1] - a.off[b] <= a.step_rows) return;  // (written by the few rows' kernel)
   float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < splits; ++s) {
-    const float2 ml = a.part_ml[(long long)s * items + item];
-    if (ml.y != 0.0f) mm = fmaxf(mm, ml.x);
-  }
-  for (int s = 0; s < splits; ++s) {
+  for (int s = 0; s < a.prompt_splits; ++s) mm = fmaxf(mm, a.part_ml[(long long)s * items + item].x);
+  for (int s = 0; s < a.prompt_splits; ++s) {
     const float2 ml = a.part_ml[(long long)s * items + item];
     if (ml.y == 0.0f) continue;
     const float f = __builtin_amdgcn_exp2f(ml.x - mm);
@@ -409,11 +547,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheAttnArgs a) 
     v[2] = fmaf(f, o.z, v[2]);
     v[3] = fmaf(f, o.w, v[3]);
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  union { uint2 u; bf16_t e[4]; } w;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) w.e[k] = f32_to_bf16(v[k] * inv);
-  *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + r * a.ldo + h * DH + d0) = w.u;
+  write_row<4>(static_cast<bf16_t*>(a.out) + r * a.ldo + h * DH + d0, v, sum);
 }
 
 }  // namespace
@@ -780,52 +914,51 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 // head, the other kernel once for each of the G heads.
 constexpr int kStepRows = 16;
 
-struct Plan {
-  int step_most, prompt_most;      // the longest sequence of each kind (0: none)
-  int tiles;                       // 16-column tiles of the longest few-row sequence
-  int step_splits, prompt_splits;  // parts of the tokens
-};
+}  // namespace
 
-Plan make_plan(const int* off, int B, int Hq, int Hkv, long long tokens, int cus) {
-  Plan p{0, 0, 1, 1, 1};
+// The few rows' workgroups: two a compute unit hold the card, each with an equal
+// stretch; fewer where the longest table gives a stretch under eight blocks or a
+// tile over 64 pieces.  Without stretches (0: a workgroup a tile, and no second
+// launch) where no table is longer than 512 tokens, or where there are four tiles
+// for each place on the card, which even out by themselves (or 2^31 blocks).
+// Prompts: two workgroups a compute unit, by splitting the tokens where there are
+// fewer tiles, 512 tokens a part at least.
+CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int Dh, bool fp4, long long tokens, int cus) {
+  CacheAttnPlan p{};
   const int G = Hq / Hkv;
-  long long step_groups = 0, prompt_groups = 0;
+  long long step_tiles = 0, prompt_tiles = 0;
   for (int b = 0; b < B; ++b) {
     const int n = off[b + 1] - off[b];
     if (n == 0) continue;
     if (n <= kStepRows) {
       p.step_most = max(p.step_most, n);
-      step_groups += (long long)((n * G + 15) / 16) * Hkv;
+      step_tiles += (long long)((n * G + 15) / 16) * Hkv;
     } else {
       p.prompt_most = max(p.prompt_most, n);
-      prompt_groups += (long long)((n + 127) / 128) * Hq;
+      prompt_tiles += (long long)((n + 127) / 128) * Hq;
     }
   }
   p.tiles = max(1, (p.step_most * G + 15) / 16);
-  auto parts = [&](long long groups, long long want, long long least) {
-    return groups == 0 ? 1 : static_cast<int>(max(1LL, min(min(want / groups, tokens / least), 64LL)));
-  };
-  p.step_splits = parts(step_groups, 2LL * cus, 256);
-  p.prompt_splits = parts(prompt_groups, 2LL * cus, 512);
+  const long long places = 2LL * cus;
+  if (step_tiles > 0 && tokens > 512 && step_tiles < 4 * places) {
+    const long long blocks = (tokens + 31) / (fp4 || Dh == 64 ? 64 : 32);
+    if (step_tiles * blocks < 1LL << 31)
+      p.groups = static_cast<int>(max(1LL, min(min(places, 64 * step_tiles), step_tiles * blocks / 8)));
+  }
+  p.prompt_splits = 1;
+  if (prompt_tiles > 0) p.prompt_splits = static_cast<int>(max(1LL, min(min(places / prompt_tiles, tokens / 512), 64LL)));
   return p;
 }
 
-}  // namespace
-
-int cache_attention_splits(const int* off, int B, int Hq, int Hkv, long long max_tokens, int cus) {
-  const Plan p = make_plan(off, B, Hq, Hkv, max_tokens, cus);
-  return max(p.step_splits, p.prompt_splits);
-}
-
-hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cus, hipStream_t s) {
-  const Plan p = make_plan(a.off, a.B, a.Hq, a.Hq / a.G, max_tokens, cus);
-  a.step_splits = p.step_splits;
-  a.prompt_splits = p.prompt_splits;
+hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
   a.tiles = p.tiles;
   a.step_rows = kStepRows;
+  a.groups = p.groups;
+  a.prompt_splits = p.prompt_splits;
   hipError_t e = hipSuccess;
+  const dim3 block(256), tiles(a.c.heads * p.tiles, 1, a.B);
   if (p.step_most > 0) {
-    const dim3 grid(p.step_splits, a.Hq / a.G * p.tiles, a.B), block(64 * kStepWaves);
+    const dim3 grid = p.groups > 0 ? dim3(p.groups) : tiles;
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, true>, grid, block, 0, s, a);
@@ -833,20 +966,28 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cu
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, false>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, false>, grid, block, 0, s, a);
   }
+  if (e == hipSuccess && p.groups > 0) {
+    if (a.fp4)
+      e = a.Dh == 128 ? launch_kernel("cache_step_join", cache_step_join_kernel<128, true>, tiles, block, 0, s, a)
+                      : launch_kernel("cache_step_join", cache_step_join_kernel<64, true>, tiles, block, 0, s, a);
+    else
+      e = a.Dh == 128 ? launch_kernel("cache_step_join", cache_step_join_kernel<128, false>, tiles, block, 0, s, a)
+                      : launch_kernel("cache_step_join", cache_step_join_kernel<64, false>, tiles, block, 0, s, a);
+  }
   if (e == hipSuccess && p.prompt_most > 0) {
-    const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.prompt_splits, a.B), block(256);
+    const dim3 grid(a.Hq, (p.prompt_most + 127) / 128 * p.prompt_splits, a.B);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, true>, grid, block, 0, s, a);
     else
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, false>, grid, block, 0, s, a);
-  }
-  if (e == hipSuccess && max(p.step_splits, p.prompt_splits) > 1) {
-    const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
-    const dim3 grid(static_cast<unsigned>((items + per - 1) / per)), block(256);
-    e = a.Dh == 128 ? launch_kernel("cache_join", cache_join_kernel<128>, grid, block, 0, s, a)
-                    : launch_kernel("cache_join", cache_join_kernel<64>, grid, block, 0, s, a);
+    if (e == hipSuccess && p.prompt_splits > 1) {
+      const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
+      const dim3 joins(static_cast<unsigned>((items + per - 1) / per));
+      e = a.Dh == 128 ? launch_kernel("cache_prompt_join", cache_prompt_join_kernel<128>, joins, block, 0, s, a)
+                      : launch_kernel("cache_prompt_join", cache_prompt_join_kernel<64>, joins, block, 0, s, a);
+    }
   }
   return e;
 }

@@ -476,15 +476,22 @@ struct CacheAttnArgs {
   float c2;               // scale log2(e)
   bool fp4;
   // set by the launch: 16-column tiles of the longest few-row sequence, the most rows
-  // of one, parts of the tokens of both kinds of sequences
-  int tiles, step_rows, step_splits, prompt_splits;
+  // of one, workgroups with a stretch of their blocks each (0: with a tile each),
+  // parts of the prompts' tokens
+  int tiles, step_rows, groups, prompt_splits;
+  float* step_o;          // [groups][2][16][Dh] sums of a stretch's first and last tile, with stretches
+  float2* step_ml;        // [groups][2][16] and (m, l)
   float* part_o;          // [part][rows][Hq][Dh] each part's sums, where there are several
   float2* part_ml;        // [part][rows][Hq] and (m, l)
   int off[MAP_CACHE_MAX_BATCH + 1];
 };
-// Parts that a call is split into (the workspace holds their sums), and the call.
-int cache_attention_splits(const int* off, int B, int Hq, int Hkv, long long max_tokens, int cus);
-hipError_t launch_cache_attention(CacheAttnArgs& a, long long max_tokens, int cus, hipStream_t s);
+// How a call is divided (the workspace holds what is joined later), and the call.
+struct CacheAttnPlan {
+  int step_most, prompt_most;  // the longest few-row sequence, the longest prompt (0: none)
+  int tiles, groups, prompt_splits;
+};
+CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int Dh, bool fp4, long long tokens, int cus);
+hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 // ---------------------------------------------------------------- teacher selection
 constexpr int kTeacherMaxLayers = 256;

@@ -1552,19 +1552,24 @@ CachePages cache_pages(const map_cache& c, const int32_t* table, int max_pages, 
   return p;
 }
 
-// The parts' sums of a split attention (at least one byte, so that 0 says invalid).
+// The sums of a divided attention (at least one byte, so that 0 says invalid).
 struct CacheAttentionWs {
-  float2* ml;
-  float* o;
+  CacheAttnPlan plan;
+  float2 *step_ml, *part_ml;
+  float *step_o, *part_o;
 };
 
 CacheAttentionWs carve_cache_attention(Carver& w, const map_cache& c, int B, int n_heads, int max_pages,
                                        const int32_t* off) {
-  const int splits = cache_attention_splits(off, B, n_heads, c.n_kv_heads, (long long)max_pages * c.page, device_cus());
-  const size_t items = splits > 1 ? (size_t)splits * off[B] * n_heads : 0;
   CacheAttentionWs t;
-  t.ml = w.take<float2>(items + 1);
-  t.o = w.take<float>(items * c.head_dim);
+  t.plan = cache_attention_plan(off, B, n_heads, c.n_kv_heads, c.head_dim, c.type == MAP_CACHE_MXFP4,
+                                (long long)max_pages * c.page, device_cus());
+  const size_t pieces = (size_t)t.plan.groups * 2 * 16;
+  const size_t items = t.plan.prompt_splits > 1 ? (size_t)t.plan.prompt_splits * off[B] * n_heads : 0;
+  t.step_ml = w.take<float2>(pieces + 1);
+  t.step_o = w.take<float>(pieces * c.head_dim);
+  t.part_ml = w.take<float2>(items);
+  t.part_o = w.take<float>(items * c.head_dim);
   return t;
 }
 
@@ -1692,10 +1697,11 @@ map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_he
   std::copy(seq_off_host, seq_off_host + B + 1, a.off);
   Carver w(ws);
   const CacheAttentionWs t = carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
-  a.part_ml = t.ml;
-  a.part_o = t.o;
-  return hip_status(
-      launch_cache_attention(a, (long long)max_pages * c->page, device_cus(), static_cast<hipStream_t>(stream)));
+  a.step_ml = t.step_ml;
+  a.step_o = t.step_o;
+  a.part_ml = t.part_ml;
+  a.part_o = t.part_o;
+  return hip_status(launch_cache_attention(a, t.plan, static_cast<hipStream_t>(stream)));
 }
 
 map_status map_set_finite_check(int enable) {
