@@ -134,7 +134,9 @@ __device__ __forceinline__ void lay_out_run(const CacheAttnArgs& a, StepRun& run
   if (t < a.B) {
     const int n = a.off[t + 1] - a.off[t], len = cache_len(a.c, t);
     run.len[t] = len;
-    if (n > 0 && n <= a.step_rows)
+    if (n > 0 && n * a.G <= 16)
+      v = visible_blocks(len - n, len, a.window, a.sinks, kb).count;
+    else if (n > 0 && n <= a.step_rows)
       for (int ct = 0; 16 * ct < n * a.G; ++ct) v += tile_blocks(a, n, len, ct, kb).count;
     v *= a.c.heads;
   }
@@ -147,7 +149,14 @@ __device__ __forceinline__ void lay_out_run(const CacheAttnArgs& a, StepRun& run
   if (lane == 63) run.wave_sum[t >> 6] = before;
   __syncthreads();
   for (int w = 0; w < (t >> 6); ++w) before += run.wave_sum[w];
-  if (t < a.B) run.begin[t + 1] = before;
+  if (t < a.B) {
+    run.begin[t + 1] = before;
+    if (blockIdx.x == 0) {  // (for the kernel that joins)
+      a.step_run[2 * t] = before - v;
+      a.step_run[2 * t + 1] = run.len[t];
+      if (t == a.B - 1) a.step_run[2 * a.B] = before;
+    }
+  }
   if (t == 0) run.begin[0] = 0;
   __syncthreads();
 }
@@ -170,10 +179,11 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
   __shared__ StepRun run_of;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lc = lane & 15, g4 = lane >> 4;
-  const bool stretch = a.groups > 0;  // otherwise a workgroup has one tile, and all of it
-  int b = blockIdx.z;
-  int x = 0, x_begin = 0, x_end = 0;
-  if (stretch) {
+  const bool stretch = a.groups > 0;  // (otherwise a workgroup has one tile, and all of it)
+  int b, x = 0, x_begin = 0, x_end = 0;
+  if (!stretch) {
+    b = blockIdx.x / (a.c.heads * a.tiles);
+  } else {
     lay_out_run(a, run_of, KB);
     const Stretches all(__builtin_amdgcn_readfirstlane(run_of.begin[a.B]), a.groups);
     x = x_begin = all.begin(blockIdx.x);
@@ -198,8 +208,8 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
       p0 -= count;
     }
   } else {
-    kvh = blockIdx.x / a.tiles;
-    ct = blockIdx.x - kvh * a.tiles;
+    kvh = blockIdx.x / a.tiles % a.c.heads;
+    ct = blockIdx.x % a.tiles;
     if (n > a.step_rows || 16 * ct >= cols) return;
   }
   const int col0 = 16 * ct, base = len - n;  // base: token of the sequence's first new row
@@ -479,16 +489,14 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
 template <int DH, bool FP4>
 __global__ __launch_bounds__(256) void cache_step_join_kernel(const CacheAttnArgs a) {
   constexpr int KB = StepShape<DH, FP4>::KB, PER = DH / 16;
-  __shared__ StepRun run_of;
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0, cols = n * a.G;
   const int kvh = blockIdx.x / a.tiles, ct = blockIdx.x - kvh * a.tiles;
   if (n > a.step_rows || 16 * ct >= cols) return;
-  lay_out_run(a, run_of, KB);
-  const int len = run_of.len[b];
-  int first = run_of.begin[b] + kvh * ((run_of.begin[b + 1] - run_of.begin[b]) / a.c.heads);
+  const int len = a.step_run[2 * b + 1];
+  int first = a.step_run[2 * b] + kvh * ((a.step_run[2 * b + 2] - a.step_run[2 * b]) / a.c.heads);
   for (int t = 0; t < ct; ++t) first += tile_blocks(a, n, len, t, KB).count;
   const int last = first + tile_blocks(a, n, len, ct, KB).count - 1;
-  const Stretches all(run_of.begin[a.B], a.groups);
+  const Stretches all(a.step_run[2 * a.B], a.groups);
   int w0 = 0, w1 = -1;  // the stretches it lies in
   if (last >= first) {
     w0 = __builtin_amdgcn_readfirstlane(all.of(first));
@@ -914,15 +922,19 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 // head, the other kernel once for each of the G heads.
 constexpr int kStepRows = 16;
 
+
 }  // namespace
 
 // The few rows' workgroups: two a compute unit hold the card, each with an equal
 // stretch; fewer where the longest table gives a stretch under eight blocks or a
 // tile over 64 pieces.  Without stretches (0: a workgroup a tile, and no second
-// launch) where no table is longer than 512 tokens, or where there are four tiles
-// for each place on the card, which even out by themselves (or 2^31 blocks).
+// launch) where no row sees over 512 tokens, or where there is a tile for each place
+// on the card: 16 single tokens over 2952 of 32 heads take 133 us that way and 141 in
+// stretches, whose tiles' ends and second launch cost what the balance does not bring
+// back unless the lengths differ (and past 2^31 blocks).
 // Prompts: two workgroups a compute unit, by splitting the tokens where there are
 // fewer tiles, 512 tokens a part at least.
+// tokens: the most that a row can see.
 CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int Dh, bool fp4, long long tokens, int cus) {
   CacheAttnPlan p{};
   const int G = Hq / Hkv;
@@ -940,7 +952,7 @@ CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int D
   }
   p.tiles = max(1, (p.step_most * G + 15) / 16);
   const long long places = 2LL * cus;
-  if (step_tiles > 0 && tokens > 512 && step_tiles < 4 * places) {
+  if (step_tiles > 0 && tokens > 512 && step_tiles < places) {
     const long long blocks = (tokens + 31) / (fp4 || Dh == 64 ? 64 : 32);
     if (step_tiles * blocks < 1LL << 31)
       p.groups = static_cast<int>(max(1LL, min(min(places, 64 * step_tiles), step_tiles * blocks / 8)));
@@ -956,9 +968,9 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipS
   a.groups = p.groups;
   a.prompt_splits = p.prompt_splits;
   hipError_t e = hipSuccess;
-  const dim3 block(256), tiles(a.c.heads * p.tiles, 1, a.B);
+  const dim3 block(256), tiles(a.c.heads * p.tiles, 1, a.B);  // the join's; the kernel itself counts them in one row
   if (p.step_most > 0) {
-    const dim3 grid = p.groups > 0 ? dim3(p.groups) : tiles;
+    const dim3 grid(p.groups > 0 ? p.groups : a.B * a.c.heads * p.tiles);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, true>, grid, block, 0, s, a);

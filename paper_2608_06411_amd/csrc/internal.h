@@ -479,6 +479,7 @@ struct CacheAttnArgs {
   // of one, workgroups with a stretch of their blocks each (0: with a tile each),
   // parts of the prompts' tokens
   int tiles, step_rows, groups, prompt_splits;
+  int32_t* step_run;      // [2 B + 1] each sequence's first block and its length; all blocks
   float* step_o;          // [groups][2][16][Dh] sums of a stretch's first and last tile, with stretches
   float2* step_ml;        // [groups][2][16] and (m, l)
   float* part_o;          // [part][rows][Hq][Dh] each part's sums, where there are several

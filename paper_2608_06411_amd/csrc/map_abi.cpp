@@ -15,6 +15,7 @@
 //                   subset (K-split GEMM + ordered sum) -> selection with
 //                   gather on the subset -> for the images whose picks are
 //                   not certified: Gram matrix -> selection with gather
+#include <limits.h>
 #include <math.h>
 #include <string.h>
 
@@ -1552,9 +1553,10 @@ CachePages cache_pages(const map_cache& c, const int32_t* table, int max_pages, 
   return p;
 }
 
-// The sums of a divided attention (at least one byte, so that 0 says invalid).
+// The sums of a divided attention.
 struct CacheAttentionWs {
   CacheAttnPlan plan;
+  int32_t* step_run;
   float2 *step_ml, *part_ml;
   float *step_o, *part_o;
 };
@@ -1566,7 +1568,8 @@ CacheAttentionWs carve_cache_attention(Carver& w, const map_cache& c, int B, int
                                 (long long)max_pages * c.page, device_cus());
   const size_t pieces = (size_t)t.plan.groups * 2 * 16;
   const size_t items = t.plan.prompt_splits > 1 ? (size_t)t.plan.prompt_splits * off[B] * n_heads : 0;
-  t.step_ml = w.take<float2>(pieces + 1);
+  t.step_run = w.take<int32_t>(2 * MAP_CACHE_MAX_BATCH + 1);
+  t.step_ml = w.take<float2>(pieces);
   t.step_o = w.take<float>(pieces * c.head_dim);
   t.part_ml = w.take<float2>(items);
   t.part_o = w.take<float>(items * c.head_dim);
@@ -1697,11 +1700,17 @@ map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_he
   std::copy(seq_off_host, seq_off_host + B + 1, a.off);
   Carver w(ws);
   const CacheAttentionWs t = carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
+  a.step_run = t.step_run;
   a.step_ml = t.step_ml;
   a.step_o = t.step_o;
   a.part_ml = t.part_ml;
   a.part_o = t.part_o;
-  return hip_status(launch_cache_attention(a, t.plan, static_cast<hipStream_t>(stream)));
+  // (the workspace is laid out for rows that see the whole table; a window needs no more of it)
+  const long long seen = window > 0 ? (long long)window + sinks : LLONG_MAX;
+  const CacheAttnPlan plan =
+      cache_attention_plan(seq_off_host, B, n_heads, c->n_kv_heads, c->head_dim, a.fp4,
+                           std::min((long long)max_pages * c->page, seen), device_cus());
+  return hip_status(launch_cache_attention(a, plan, static_cast<hipStream_t>(stream)));
 }
 
 map_status map_set_finite_check(int enable) {
