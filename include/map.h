@@ -501,8 +501,9 @@ map_status map_selection_status(const void* ws, int32_t* status_out, void* strea
  * (enable != 0), map_score, map_similarity, map_select, map_prune,
  * map_prune_assemble, map_prune_noalloc, map_teacher, map_train_step and
  * map_decoder_layer first scan their floating-point inputs (activations,
- * weights, scores, similarities, attention, teacher distributions; the cache
- * calls, whose inputs may hold anything in what no row sees, do not) on
+ * weights, scores, similarities, attention, teacher distributions; not
+ * map_qk_norm_rope's and the cache calls', whose inputs may hold anything where
+ * no row sees it) on
  * `stream` for infinities and NaNs, wait for the scan (the call then blocks
  * until the stream has passed it, so it cannot be captured in a graph) and
  * return MAP_ERR_NONFINITE, having enqueued nothing else, if it finds one.

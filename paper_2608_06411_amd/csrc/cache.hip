@@ -1,12 +1,13 @@
 // Rows of keys and values to the pages of a cache and back.
 //
-// Both directions move 16 bytes (eight bf16 values) a lane.  A workgroup takes
-// 16 consecutive new rows of one sequence and runs through their (head, row)
-// pairs with the row fastest: the rows of a head lie next to each other in a
-// page, so what a workgroup writes (reads) there at a time is contiguous, and a
-// cache line of 4-bit codes or of scale bytes, which holds several tokens, is
-// written by one compute unit and not by several dies' L2 caches in turn.
-// Bound: the bytes, 2 rows (keys, values) read and written.
+// Both directions move 16 bytes (eight bf16 values) a lane, head_dim / 8 lanes a
+// (row, head) pair.  A workgroup takes up to 16 consecutive new rows of one
+// sequence, each lane one row and every so many heads of it: the rows of a head lie
+// next to each other in a page, so what a workgroup writes (reads) there at a time
+// is contiguous, and a cache line of 4-bit codes or of scale bytes, which holds
+// several tokens, is written by one compute unit and not by several dies' L2 caches
+// in turn; and a lane looks its row's page up once.  Bound: the bytes, 2 rows
+// (keys, values) read and written; the next pair is loaded before one is stored.
 //
 // 4 bits: the largest magnitude of 32 values (four lanes) has the bits of a
 // bf16 number, so the smallest e with max <= 7 * 2^e is its exponent minus 2,
@@ -50,37 +51,56 @@ __device__ __forceinline__ uint32_t fp4_codes(const Eight& v, uint32_t byte) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2_t, v.w[3]), s, 3);
 }
 
+// The row (of its tile) and the heads of a lane's pair: rows = the tile's rows
+// rounded up to a power of two side by side, the other lanes further heads.
+struct Pair {
+  int row, head, step;  // head, head + step, ...
+  __device__ __forceinline__ Pair(int nt, int pairs, int lanes, int part, int parts) {
+    const int shift = nt > 8 ? 4 : nt > 4 ? 3 : nt > 2 ? 2 : nt > 1 ? 1 : 0, g = threadIdx.x / lanes;
+    row = g & ((1 << shift) - 1);
+    head = (g >> shift) + part * (pairs >> shift);
+    step = parts * (pairs >> shift);
+  }
+};
+
 template <int DH, bool FP4>
 __global__ __launch_bounds__(NT) void cache_append_kernel(const CacheRowsArgs a) {
   constexpr int LPH = DH / 8, PAIRS = NT / LPH;  // lanes a (head, row) pair, pairs at a time
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
   const int t0 = blockIdx.x * kTile, nt = min(kTile, n - t0);
   if (nt <= 0) return;
-  const int first = cache_len(a.c, b) - n;  // token of the sequence's first row
-  const int l = threadIdx.x % LPH;
-  for (int it = blockIdx.y * PAIRS + threadIdx.x / LPH; it < nt * a.c.heads; it += a.parts * PAIRS) {
-    const int h = it / nt, i = t0 + it - h * nt, j = first + i;
-    if (j < 0) continue;
-    const int page = cache_page(a.c, b, j);
-    if (page < 0) continue;
+  const Pair p(nt, PAIRS, LPH, blockIdx.y, a.parts);
+  const int l = threadIdx.x % LPH, i = t0 + p.row, j = cache_len(a.c, b) - n + i;
+  // (a pair's lanes are all here or all away: the exchange below stays within them)
+  const int page = p.row < nt && j >= 0 ? cache_page(a.c, b, j) : -1;
+  if (page < 0) return;
+  const bf16_t* src_k = static_cast<const bf16_t*>(a.k) + (r0 + i) * a.ldk + 8 * l;
+  const bf16_t* src_v = static_cast<const bf16_t*>(a.v) + (r0 + i) * a.ldv + 8 * l;
+  Eight k, v;
+  if (p.head < a.c.heads) {
+    k.u = *reinterpret_cast<const uint4*>(src_k + p.head * DH);
+    v.u = *reinterpret_cast<const uint4*>(src_v + p.head * DH);
+  }
+  for (int h = p.head; h < a.c.heads; h += p.step) {
+    const Eight kc = k, vc = v;
+    if (h + p.step < a.c.heads) {
+      k.u = *reinterpret_cast<const uint4*>(src_k + (h + p.step) * DH);
+      v.u = *reinterpret_cast<const uint4*>(src_v + (h + p.step) * DH);
+    }
     const long long row = cache_row(a.c, page, h, j);
-    Eight k, v;
-    k.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.k) + (r0 + i) * a.ldk + h * DH + 8 * l);
-    v.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.v) + (r0 + i) * a.ldv + h * DH + 8 * l);
     if constexpr (!FP4) {
-      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.c.k) + row * DH + 8 * l) = k.u;
-      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.c.v) + row * DH + 8 * l) = v.u;
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.c.k) + row * DH + 8 * l) = kc.u;
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.c.v) + row * DH + 8 * l) = vc.u;
     } else {
-      // (a pair's lanes are all here or all away: the exchange stays within them)
-      uint32_t mk = amax_bits(k), mv = amax_bits(v);
+      uint32_t mk = amax_bits(kc), mv = amax_bits(vc);
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1) {
         mk = max(mk, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mk), o, 64)));
         mv = max(mv, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mv), o, 64)));
       }
       const uint32_t bk = fp4_byte(mk), bv = fp4_byte(mv);
-      static_cast<uint32_t*>(a.c.k)[row * LPH + l] = fp4_codes(k, bk);
-      static_cast<uint32_t*>(a.c.v)[row * LPH + l] = fp4_codes(v, bv);
+      static_cast<uint32_t*>(a.c.k)[row * LPH + l] = fp4_codes(kc, bk);
+      static_cast<uint32_t*>(a.c.v)[row * LPH + l] = fp4_codes(vc, bv);
       if ((l & 3) == 0) {
         a.c.ks[row * (DH / 32) + l / 4] = static_cast<uint8_t>(bk);
         a.c.vs[row * (DH / 32) + l / 4] = static_cast<uint8_t>(bv);
@@ -95,39 +115,62 @@ __global__ __launch_bounds__(NT) void cache_read_kernel(const CacheRowsArgs a) {
   const int b = blockIdx.z, r0 = a.off[b], n = a.off[b + 1] - r0;
   const int t0 = blockIdx.x * kTile, nt = min(kTile, n - t0);
   if (nt <= 0) return;
-  const int len = cache_len(a.c, b), l = threadIdx.x % LPH;
-  for (int it = blockIdx.y * PAIRS + threadIdx.x / LPH; it < nt * a.c.heads; it += a.parts * PAIRS) {
-    const int h = it / nt, i = t0 + it - h * nt, j = a.slots ? a.slots[r0 + i] : i;
-    const int page = j >= 0 && j < len ? cache_page(a.c, b, j) : -1;
-    Eight k, v;
-    k.u = v.u = make_uint4(0u, 0u, 0u, 0u);
-    if (page >= 0) {
-      const long long row = cache_row(a.c, page, h, j);
-      if constexpr (!FP4) {
-        k.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.k) + row * DH + 8 * l);
-        v.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.v) + row * DH + 8 * l);
-      } else {
-        k.u = fp4_eight(static_cast<const uint32_t*>(a.c.k)[row * LPH + l], fp4_scale(a.c.ks[row * (DH / 32) + l / 4]));
-        v.u = fp4_eight(static_cast<const uint32_t*>(a.c.v)[row * LPH + l], fp4_scale(a.c.vs[row * (DH / 32) + l / 4]));
-      }
+  const Pair p(nt, PAIRS, LPH, blockIdx.y, a.parts);
+  if (p.row >= nt) return;
+  const int l = threadIdx.x % LPH, i = t0 + p.row, j = a.slots ? a.slots[r0 + i] : i;
+  const int page = j >= 0 && j < cache_len(a.c, b) ? cache_page(a.c, b, j) : -1;
+  bf16_t* dst_k = static_cast<bf16_t*>(a.k) + (r0 + i) * a.ldk + 8 * l;
+  bf16_t* dst_v = static_cast<bf16_t*>(a.v) + (r0 + i) * a.ldv + 8 * l;
+  Eight k, v;
+  uint32_t kw = 0, vw = 0, kb = 0, vb = 0;
+  k.u = v.u = make_uint4(0u, 0u, 0u, 0u);
+  auto load = [&](int h) {  // (no page: zeros stay)
+    if (page < 0 || h >= a.c.heads) return;
+    const long long row = cache_row(a.c, page, h, j);
+    if constexpr (!FP4) {
+      k.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.k) + row * DH + 8 * l);
+      v.u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.c.v) + row * DH + 8 * l);
+    } else {
+      kw = static_cast<const uint32_t*>(a.c.k)[row * LPH + l];
+      vw = static_cast<const uint32_t*>(a.c.v)[row * LPH + l];
+      kb = a.c.ks[row * (DH / 32) + l / 4];
+      vb = a.c.vs[row * (DH / 32) + l / 4];
     }
-    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.k) + (r0 + i) * a.ldk + h * DH + 8 * l) = k.u;
-    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.v) + (r0 + i) * a.ldv + h * DH + 8 * l) = v.u;
+  };
+  load(p.head);
+  for (int h = p.head; h < a.c.heads; h += p.step) {
+    Eight kc = k, vc = v;
+    if constexpr (FP4) {
+      kc.u = fp4_eight(kw, fp4_scale(kb));
+      vc.u = fp4_eight(vw, fp4_scale(vb));
+    }
+    load(h + p.step);
+    *reinterpret_cast<uint4*>(dst_k + h * DH) = kc.u;
+    *reinterpret_cast<uint4*>(dst_v + h * DH) = vc.u;
   }
 }
 
-// Tiles of the longest sequence, and workgroups a tile.
-dim3 rows_grid(CacheRowsArgs& a) {
-  int most = 0;
-  for (int b = 0; b < a.B; ++b) most = max(most, a.off[b + 1] - a.off[b]);
-  a.parts = 1;
-  return dim3((most + kTile - 1) / kTile, a.parts, a.B);
+// Tiles of the longest sequence, and workgroups a tile, so that there are about
+// `want` of them (one round of heads each at least).  Writing gains by many short
+// ones, reading by few long ones (11776 rows of 32 heads in bf16: append 102 us with
+// 512 wanted, 82 with 4096, 78 with 8192; read 76, 82, 82).
+dim3 rows_grid(CacheRowsArgs& a, long long want) {
+  long long most = 0, tiles = 0;
+  for (int b = 0; b < a.B; ++b) {
+    const int n = a.off[b + 1] - a.off[b];
+    most = max(most, (long long)n);
+    tiles += (n + kTile - 1) / kTile;
+  }
+  const int side = most > 8 ? 16 : most > 4 ? 8 : most > 2 ? 4 : most > 1 ? 2 : 1;  // rows side by side
+  const int heads = NT / (a.Dh / 8) / side, rounds = (a.c.heads + heads - 1) / heads;
+  a.parts = static_cast<int>(max(1LL, min((long long)rounds, want / max(tiles, 1LL))));
+  return dim3(static_cast<unsigned>((most + kTile - 1) / kTile), a.parts, a.B);
 }
 
 }  // namespace
 
 hipError_t launch_cache_append(CacheRowsArgs& a, hipStream_t s) {
-  const dim3 grid = rows_grid(a), block(NT);
+  const dim3 grid = rows_grid(a, 8192), block(NT);
   if (a.fp4)
     return a.Dh == 128 ? launch_kernel("cache_append", cache_append_kernel<128, true>, grid, block, 0, s, a)
                        : launch_kernel("cache_append", cache_append_kernel<64, true>, grid, block, 0, s, a);
@@ -136,7 +179,7 @@ hipError_t launch_cache_append(CacheRowsArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_cache_read(CacheRowsArgs& a, hipStream_t s) {
-  const dim3 grid = rows_grid(a), block(NT);
+  const dim3 grid = rows_grid(a, 512), block(NT);
   if (a.fp4)
     return a.Dh == 128 ? launch_kernel("cache_read", cache_read_kernel<128, true>, grid, block, 0, s, a)
                        : launch_kernel("cache_read", cache_read_kernel<64, true>, grid, block, 0, s, a);

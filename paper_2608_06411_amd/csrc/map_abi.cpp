@@ -15,7 +15,6 @@
 //                   subset (K-split GEMM + ordered sum) -> selection with
 //                   gather on the subset -> for the images whose picks are
 //                   not certified: Gram matrix -> selection with gather
-#include <limits.h>
 #include <math.h>
 #include <string.h>
 
@@ -1659,11 +1658,14 @@ map_status map_cache_read(const map_cache* c, map_dtype dt, int B, const int32_t
   return hip_status(launch_cache_read(a, static_cast<hipStream_t>(stream)));
 }
 
+static bool valid_cache_attention(const map_cache* c, int B, int n_heads, int max_pages, const int32_t* off) {
+  return valid_cache(c) && valid_table(*c, max_pages) && valid_rows(off, B) && n_heads >= 1 && n_heads <= 1024 &&
+         n_heads % c->n_kv_heads == 0;
+}
+
 size_t map_cache_attention_workspace(const map_cache* c, int B, int n_heads, int max_pages,
                                      const int32_t* seq_off_host) {
-  if (!valid_cache(c) || !valid_table(*c, max_pages) || !valid_rows(seq_off_host, B) || n_heads < 1 ||
-      n_heads > 1024 || n_heads % c->n_kv_heads != 0)
-    return 0;
+  if (!valid_cache_attention(c, B, n_heads, max_pages, seq_off_host)) return 0;
   Carver w(nullptr);
   carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
   return w.off;
@@ -1673,14 +1675,15 @@ map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_he
                                int max_pages, const int32_t* len, const void* q, int64_t ldq,
                                const int32_t* seq_off_host, float scale, int window, int sinks, void* out,
                                int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
-  const size_t need = map_cache_attention_workspace(c, B, n_heads, max_pages, seq_off_host);
-  if (!valid_dtype(dt) || need == 0 || !table || !len || !q || !out || !aligned16({q, out}) || !(scale > 0.0f && scale < 1e30f) ||
-      window < 0 || sinks < 0)
+  if (!valid_dtype(dt) || !valid_cache_attention(c, B, n_heads, max_pages, seq_off_host) || !table || !len || !q ||
+      !out || !aligned16({q, out}) || !(scale > 0.0f && scale < 1e30f) || window < 0 || sinks < 0)
     return MAP_ERR_INVALID_ARG;
   const int64_t row = (int64_t)n_heads * c->head_dim;
   if (!valid_ld(ldq, row, 2) || !valid_ld(ldo, row, 2)) return MAP_ERR_INVALID_ARG;
   if (dt != MAP_BF16) return MAP_ERR_UNSUPPORTED;
-  const map_status ws_ok = check_ws(ws, ws_bytes, need);
+  Carver w(ws);
+  const CacheAttentionWs t = carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
+  const map_status ws_ok = check_ws(ws, ws_bytes, w.off);
   if (ws_ok != MAP_OK) return ws_ok;
   if (seq_off_host[B] == 0) return MAP_OK;
   CacheAttnArgs a;
@@ -1693,23 +1696,22 @@ map_status map_cache_attention(const map_cache* c, map_dtype dt, int B, int n_he
   a.Hq = n_heads;
   a.G = n_heads / c->n_kv_heads;
   a.Dh = c->head_dim;
-  a.window = window;
+  const long long most = (long long)max_pages * c->page;
+  a.window = window < most ? window : 0;  // (one that no sequence outgrows is none)
   a.sinks = sinks;
   a.c2 = static_cast<float>(scale * 1.4426950408889634);
   a.fp4 = c->type == MAP_CACHE_MXFP4;
   std::copy(seq_off_host, seq_off_host + B + 1, a.off);
-  Carver w(ws);
-  const CacheAttentionWs t = carve_cache_attention(w, *c, B, n_heads, max_pages, seq_off_host);
   a.step_run = t.step_run;
   a.step_ml = t.step_ml;
   a.step_o = t.step_o;
   a.part_ml = t.part_ml;
   a.part_o = t.part_o;
   // (the workspace is laid out for rows that see the whole table; a window needs no more of it)
-  const long long seen = window > 0 ? (long long)window + sinks : LLONG_MAX;
-  const CacheAttnPlan plan =
-      cache_attention_plan(seq_off_host, B, n_heads, c->n_kv_heads, c->head_dim, a.fp4,
-                           std::min((long long)max_pages * c->page, seen), device_cus());
+  CacheAttnPlan plan = t.plan;
+  if (a.window > 0 && (long long)a.window + sinks < most)
+    plan = cache_attention_plan(seq_off_host, B, n_heads, c->n_kv_heads, c->head_dim, a.fp4, (long long)a.window + sinks,
+                                device_cus());
   return hip_status(launch_cache_attention(a, plan, static_cast<hipStream_t>(stream)));
 }
 

@@ -12,6 +12,8 @@
 // The angle goes through turns, in float64: pos * turns[i] minus its nearest
 // whole number is exact but for the product's rounding (a turn's 2^-53 times
 // the position), and the sine of the float32 rest is within a few 2^-24.
+// Bound: the bytes.  37600 rows of 32 heads in bf16 (616 MB in and out): 116 us,
+// 5.3 TB/s, the rate of a large copy.
 #include "internal.h"
 
 namespace mapk {
@@ -118,10 +120,12 @@ __global__ __launch_bounds__(NT) void qk_norm_rope_kernel(const QkRopeArgs a) {
 
 hipError_t launch_qk_norm_rope(map_dtype dt, QkRopeArgs& a, hipStream_t s) {
   const int per_wave = 64 / (a.Dh / 16), chunks = (a.Hq + a.Hkv + per_wave - 1) / per_wave;
-  a.parts = 1;
+  // A wave takes a whole row's heads, so that its angles are formed once; with few
+  // rows, a share of them, so that there are about 2048 waves (224 rows of 64 heads in
+  // float32: 10.7 us with a wave a row, 5.6 so).
+  a.parts = static_cast<int>(max(1LL, min((long long)chunks, 2048LL / a.R)));
   const long long waves = (long long)a.R * a.parts;
   const dim3 grid(static_cast<unsigned>((waves + kWaves - 1) / kWaves));
-  (void)chunks;
   if (dt == MAP_BF16)
     return a.Dh == 128 ? launch_kernel("qk_norm_rope", qk_norm_rope_kernel<bf16_t, 128>, grid, dim3(NT), 0, s, a)
                        : launch_kernel("qk_norm_rope", qk_norm_rope_kernel<bf16_t, 64>, grid, dim3(NT), 0, s, a);

@@ -481,3 +481,103 @@ def test_a_decoder_layers_attention_from_the_cache():
     # the same stored bf16 intermediates by other sums: the layer's own bar
     du, dw = (got.double() - X.double()), (want.double() - X.double())
     assert float((du - dw).norm() / dw.norm()) <= 1e-2
+
+
+# ------------------------------------------------ how a call is divided
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dh,heads,G,page,n,past,window,sinks", [
+    (64, 2, 2, 16, [1, 3, 1, 0, 2], [3000, 5, 0, 700, 1200], 0, 0),       # stretches over sequences of very different lengths
+    (128, 1, 7, 64, [5, 1, 4], [900, 2500, 0], 0, 0),                     # ... over tiles of 16 of 35 (row, head) pairs
+    (128, 2, 4, 32, [9, 16, 1], [1500, 40, 600], 300, 20),                # ... and a window's two ranges
+    (64, 1, 3, 128, [1, 40, 2, 130], [2000, 1800, 600, 0], 0, 0),         # single tokens and prompts in one call
+    (128, 1, 2, 16, [17, 1], [1400, 1300], 200, 4),
+])
+def test_attention_divided(kind, dh, heads, G, page, n, past, window, sinks):
+    announce(f"cache attention divided {kind} {heads * G}/{heads} x {dh}, {n} behind {past}, window {window}")
+    b = Batch(kind, dh, heads, page, n, past, seed=sum(past) + dh, wide=5, fill=float("nan"))
+    b.append()
+    q = b.rows(b.off[-1], heads=heads * G, scale=1.5)
+    b.check(q, window, sinks)
+    # a length past the table, one of zero, one of a sequence shorter than its rows
+    b.lens = b.lens.clone()
+    b.lens[0], b.lens[1] = 2 ** 30, min(2, int(b.lens[1]))
+    b.oracle.rows.update({(p, s): (np.zeros((heads, dh)), np.zeros((heads, dh)))
+                          for p, s in [(int(b.table[0, j // page]), j % page) for j in range(n[0] + past[0], b.table.shape[1] * page)]})
+    for t, w in ((b.cache.k, 0), (b.cache.v, 0), (b.cache.k_scale, 127), (b.cache.v_scale, 127)):
+        if t is not None:
+            for j in range(n[0] + past[0], b.table.shape[1] * page):
+                t[int(b.table[0, j // page]), :, j % page] = w
+    b.check(q, window, sinks)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_hidden_values_in_long_caches(kind):
+    """NaN between the first tokens and the windows, and in the last row's own
+    token, where the few rows' blocks lie in several stretches."""
+    announce(f"cache attention {kind}, NaN hidden in a long cache")
+    b = Batch(kind, 64, 1, 16, [5, 1], [1500, 900], seed=21)
+    k, v = b.rows(6), b.rows(6)
+    b.append(k, v)
+    q = b.rows(6, heads=2)
+    clean = _f64(b.attend(q, 400, 3))
+    v[4, 0, 7] = float("nan")
+    b.append(k, v)
+    page, place = int(b.table[0, 700 // 16]), 700 % 16
+    if kind == "bf16":
+        b.cache.v[page, 0, place, 9] = float("inf")
+        b.cache.k[page, 0, place, 3] = float("nan")
+    else:
+        b.cache.v_scale[page, 0, place, 0] = b.cache.k_scale[page, 0, place, 1] = 255
+    got = _f64(b.attend(q, 400, 3))
+    assert not np.isfinite(got[4]).all()
+    np.testing.assert_array_equal(got[[0, 1, 2, 3, 5]], clean[[0, 1, 2, 3, 5]])
+
+
+def test_prompt_behind_more_blocks_than_pages_held():
+    """A prompt's tokens past 256 blocks of 64 (the table's entries are brought
+    256 blocks at a time), with as many heads as keep the tokens in one part."""
+    mp, dev = _mp(), device()
+    announce("cache prompt past 256 blocks")
+    past, n, H, dh = 16500, 20, 512, 64
+    for kind in KINDS:
+        g = torch.Generator(device=dev).manual_seed(5)
+        cache = mp.KVCache(140, 128, 1, dh, kind, device=dev)
+        table = torch.randperm(140, generator=torch.Generator().manual_seed(1))[None, :130].to(torch.int32).to(dev)
+        lens = torch.tensor([past + n], dtype=torch.int32, device=dev)
+        k, v = (torch.randn(past + n, 1, dh, generator=g, device=dev).bfloat16() for _ in range(2))
+        mp.map_cache_append(cache, table, lens, k, v, [0, past + n])
+        k, v = mp.map_cache_read(cache, table, lens, [0, past + n])
+        q = torch.randn(n, H, dh, generator=g, device=dev).bfloat16()
+        for window, sinks in ((0, 0), (16400, 70)):
+            o = mp.map_cache_attention(cache, table, lens, q, [0, n], window=window, sinks=sinks)
+            at = past + torch.arange(n, device=dev)[:, None]
+            j = torch.arange(past + n, device=dev)[None]
+            hide = (j > at) | ((at - j >= window) & (j >= sinks) if window else j < 0)
+            for h in (0, 255, 511):
+                z = (q[:, h].double() @ k[:, 0].double().T.contiguous()) / dh ** 0.5
+                p = torch.softmax(z.masked_fill(hide, -float("inf")), 1)
+                want, spread = p @ v[:, 0].double(), p @ v[:, 0].double().abs()
+                assert ((o[:, h].double() - want).abs() <= U[torch.bfloat16] * (want.abs() + spread) + spread * 2.0 ** -10).all()
+
+
+def test_two_calls_at_once():
+    """Two streams, two workspaces, one cache: both calls' results are what each
+    gives alone."""
+    mp, dev = _mp(), device()
+    announce("cache, two calls at once")
+    b = Batch("mxfp4", 128, 2, 32, [1, 2, 1], [2500, 900, 40], seed=31)
+    c = Batch("bf16", 128, 2, 32, [40, 1], [1200, 3000], seed=32)
+    b.append()
+    c.append()
+    qs = [b.rows(4, heads=4).to(dev), c.rows(41, heads=4).to(dev)]
+    alone = [b.attend(qs[0]), c.attend(qs[1])]
+    args = [(x.cache, x.table.to(dev), x.lens.to(dev), q, mp.SeqOffsets(x.off)) for x, q in ((b, qs[0]), (c, qs[1]))]
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(8):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(mp.map_cache_attention(*args[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(o, alone[i]) for o in outs[i])
