@@ -168,7 +168,7 @@ def _need(t: torch.Tensor, name: str, shape, dtype, device):
     (device None: only checked to be a GPU device, by _on_gpu)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != dtype or t.shape != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)}, got "
                          f"{t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
     if device is not None and t.device != device:
@@ -713,10 +713,14 @@ def _rows_ld(t, name: str, rows: int, heads: int, dh: int, dtype, device) -> int
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     shape = t.shape
-    if t.dtype != dtype or len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != dh:
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != dh:
         raise ValueError(f"{name}: expected {dtype} [at least {rows}, {heads}, {dh}], got {t.dtype} {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+    if t.is_contiguous():
+        row = heads * dh  # (a multiple of 16 bytes: head_dim is one of 16 values)
+        if t.data_ptr() % 16 == 0:
+            return row
     row, head, one = t.stride()
     if shape[0] <= 1:
         row = heads * dh
@@ -833,7 +837,7 @@ def map_cache_read(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, seq_
     if k_out is None:
         k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+        v_out = torch.empty_like(k_out, memory_format=torch.contiguous_format)
     if off.rows > 0:
         _launch("map_cache_read", lib().map_cache_read, cache.device, cache._ref, MAP_BF16, off.B, table.data_ptr(), wide,
                 lens.data_ptr(), None if slots is None else slots.data_ptr(), off._arr, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv)
