@@ -545,11 +545,12 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheAttnA
     if (b + s < a.B && a.off[b + s] <= r) b += s;
   if (a.off[b + 1] - a.off[b] <= a.step_rows) return;  // (written by the few rows' kernel)
   float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
   for (int s = 0; s < a.prompt_splits; ++s) mm = fmaxf(mm, a.part_ml[(long long)s * items + item].x);
+#pragma unroll 8  // (their loads together: no branch on a part that saw nothing, whose sums are zeros)
   for (int s = 0; s < a.prompt_splits; ++s) {
     const float2 ml = a.part_ml[(long long)s * items + item];
-    if (ml.y == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - mm);
+    const float f = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mm);
     const float4 o = *reinterpret_cast<const float4*>(a.part_o + ((long long)s * items + item) * DH + d0);
     sum = fmaf(f, ml.y, sum);
     v[0] = fmaf(f, o.x, v[0]);
