@@ -571,10 +571,11 @@ namespace {
 // barrier a block, the next block on its way under this one's products: bf16
 // pages by direct loads, 4-bit pages through registers, widened once for all the
 // workgroup's rows.  A wave brings the 16 tokens that one table entry names.
-// Bound: the two waves of a SIMD share its matrix and vector units, about a third of
-// the time each, and overlap in part.  2944 rows of 32 heads, causal: 87 us (71 GFLOP
-// of visible scores, 0.82 PFLOP/s); two prompts of 4700 rows, 28 heads over 4 in 4
-// bits, window 1152: 206 us (0.69 PFLOP/s).
+// Bound: the clock, which a full card lowers to 1.6 GHz; a block takes a wave 3600
+// clocks, 1024 of them matrix instructions, 880 the issue of its loads, and the two
+// waves of a SIMD overlap in part.  2944 rows of 32 heads, causal: 88 us (71 GFLOP of
+// visible scores, 0.81 PFLOP/s); two prompts of 4700 rows, 28 heads over 4 in 4 bits,
+// window 1152: 206 us (0.69 PFLOP/s).  64 rows a wave, one wave a SIMD: 143 for 89 us.
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 constexpr int kKeys = 64;
 
