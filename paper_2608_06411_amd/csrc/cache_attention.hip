@@ -942,7 +942,8 @@ constexpr int kStepRows = 16;
 // launch) where no row sees over 512 tokens, or where there is a tile for each place
 // on the card: 16 single tokens over 2952 of 32 heads take 133 us that way and 141 in
 // stretches, whose tiles' ends and second launch cost what the balance does not bring
-// back unless the lengths differ (and past 2^31 blocks).
+// back unless the lengths differ (and where the run might pass 2^30 blocks, which are
+// counted in an int; a window may bring it back, so the workspace has the room).
 // Prompts: two workgroups a compute unit, by splitting the tokens where there are
 // fewer tiles, 512 tokens a part at least.
 // tokens: the most that a row can see.
@@ -965,8 +966,8 @@ CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int D
   const long long places = 2LL * cus;
   if (step_tiles > 0 && tokens > 512 && step_tiles < places) {
     const long long blocks = (tokens + 31) / (fp4 || Dh == 64 ? 64 : 32);
-    if (step_tiles * blocks < 1LL << 31)
-      p.groups = static_cast<int>(max(1LL, min(min(places, 64 * step_tiles), step_tiles * blocks / 8)));
+    p.groups = static_cast<int>(max(1LL, min(min(places, 64 * step_tiles), step_tiles * blocks / 8)));
+    p.run_fits = step_tiles * blocks < 1LL << 30;
   }
   p.prompt_splits = 1;
   if (prompt_tiles > 0) p.prompt_splits = static_cast<int>(max(1LL, min(min(places / prompt_tiles, tokens / 512), 64LL)));
@@ -974,14 +975,15 @@ CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int D
 }
 
 hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
+  const int groups = p.run_fits ? p.groups : 0;
   a.tiles = p.tiles;
   a.step_rows = kStepRows;
-  a.groups = p.groups;
+  a.groups = groups;
   a.prompt_splits = p.prompt_splits;
   hipError_t e = hipSuccess;
   const dim3 block(256), tiles(a.c.heads * p.tiles, 1, a.B);  // the join's; the kernel itself counts them in one row
   if (p.step_most > 0) {
-    const dim3 grid(p.groups > 0 ? p.groups : a.B * a.c.heads * p.tiles);
+    const dim3 grid(groups > 0 ? groups : a.B * a.c.heads * p.tiles);
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, true>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, true>, grid, block, 0, s, a);
@@ -989,7 +991,7 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipS
       e = a.Dh == 128 ? launch_kernel("cache_step", cache_step_kernel<128, false>, grid, block, 0, s, a)
                       : launch_kernel("cache_step", cache_step_kernel<64, false>, grid, block, 0, s, a);
   }
-  if (e == hipSuccess && p.groups > 0) {
+  if (e == hipSuccess && groups > 0) {
     if (a.fp4)
       e = a.Dh == 128 ? launch_kernel("cache_step_join", cache_step_join_kernel<128, true>, tiles, block, 0, s, a)
                       : launch_kernel("cache_step_join", cache_step_join_kernel<64, true>, tiles, block, 0, s, a);

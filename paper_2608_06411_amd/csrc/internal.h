@@ -490,6 +490,7 @@ struct CacheAttnArgs {
 struct CacheAttnPlan {
   int step_most, prompt_most;  // the longest few-row sequence, the longest prompt (0: none)
   int tiles, groups, prompt_splits;
+  bool run_fits;  // the stretches' blocks can be counted: without it a workgroup takes a tile
 };
 CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int Dh, bool fp4, long long tokens, int cus);
 hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);

@@ -161,3 +161,14 @@ def test_binding_refuses_bad_rotations():
     for sec in ([64, 1], [], [10, 10, 10, 10, 24], [-1, 65]):
         with pytest.raises(ValueError, match="sections"):
             mp.RopeParams(128, sections=sec)
+
+
+def test_attention_workspace_grows_with_the_table():
+    # The calls with a window run on the workspace of their table: one for a longer table serves a shorter view of it,
+    # up to the longest table that is allowed (2^30 tokens, whose blocks over 64 tiles pass an int's count).
+    off = _off(*range(9))  # eight single tokens
+    for kind in (bd.MAP_CACHE_BF16, bd.MAP_CACHE_MXFP4):
+        c = _cache(type=kind, page=128, n_kv_heads=16)
+        sizes = [bd.lib().map_cache_attention_workspace(ctypes.byref(c), 8, 16, 1 << w, off) for w in range(24)]
+        assert sizes[0] > 0 and sizes == sorted(sizes)
+        assert bd.lib().map_cache_attention_workspace(ctypes.byref(c), 8, 16, (1 << 23) + 1, off) == 0
