@@ -766,10 +766,12 @@ def map_qk_norm_rope(rope: RopeParams, q: torch.Tensor, k: torch.Tensor, pos: to
     for one axis), in one pass.  q and k may be views into a wider row (a qkv
     product); q_out and k_out may be q and k themselves.  Returns (q_out, k_out)."""
     R, Hq, dh = _dims(q, "q", 3)
-    _, Hk, _ = _dims(k, "k", 3)
+    Rk, Hk, _ = _dims(k, "k", 3)
     dt, dev, dtype = _dtype_code(q), q.device, q.dtype
     if dh != rope.head_dim:
         raise ValueError(f"q: heads of {dh}, the rotation is for {rope.head_dim}")
+    if Rk != R:
+        raise ValueError(f"k: {Rk} rows, q has {R}")
     axes = len(rope.sections)
     if isinstance(pos, torch.Tensor) and pos.dim() == 1 and axes == 1:
         pos = pos[None]
@@ -868,8 +870,8 @@ def map_cache_attention(cache: KVCache, table: torch.Tensor, lens: torch.Tensor,
     ldo = heads * dh if out is None else _rows_ld(out, "out", off.rows, heads, dh, torch.bfloat16, cache.device)
     if heads % cache.n_kv_heads or not 1 <= heads <= 1024:
         raise ValueError(f"q: {heads} heads over {cache.n_kv_heads} key/value heads")
-    if window < 0 or sinks < 0:
-        raise ValueError("window and sinks must not be negative")
+    if not 0 <= window < 1 << 31 or not 0 <= sinks < 1 << 31:
+        raise ValueError(f"window and sinks must not be negative or pass 31 bits, got {window} and {sinks}")
     _on_gpu(q, "q")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)

@@ -172,3 +172,16 @@ def test_attention_workspace_grows_with_the_table():
         sizes = [bd.lib().map_cache_attention_workspace(ctypes.byref(c), 8, 16, 1 << w, off) for w in range(24)]
         assert sizes[0] > 0 and sizes == sorted(sizes)
         assert bd.lib().map_cache_attention_workspace(ctypes.byref(c), 8, 16, (1 << 23) + 1, off) == 0
+
+
+def test_binding_refuses_rows_that_differ():
+    rp, pos = mp.RopeParams(64), torch.zeros(5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="6 rows"):  # (its last row would come back unwritten)
+        mp.map_qk_norm_rope(rp, torch.zeros(5, 4, 64), torch.zeros(6, 2, 64), pos)
+
+
+@pytest.mark.parametrize("bad", [dict(window=1 << 31), dict(sinks=(1 << 32) + 4), dict(sinks=-1)])
+def test_binding_refuses_sizes_past_an_int(bad):
+    d = _cpu("bf16")
+    with pytest.raises(ValueError, match="31 bits"):
+        mp.map_cache_attention(d["cache"], d["table"], d["lens"], d["q"], d["off"], **bad)
