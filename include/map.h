@@ -458,8 +458,9 @@ map_status map_cache_read(const map_cache* c, map_dtype dt, int B, const int32_t
  * -3e38 weighs nothing.
  * q [rows][n_heads][head_dim] bf16, rows ldq apart; out likewise, ldo apart;
  * n_heads a multiple of n_kv_heads, at most 1024; 0 < scale < 1e30.  Scores, the softmax and its
- * sums are float32; probabilities enter the second product as bf16, and so do
- * the 4-bit values (exactly).  out must not overlap q.
+ * sums are float32; probabilities enter the second product as two bf16 numbers each (2^-17 of their
+ * value) for sequences of up to 16 new rows, as one (2^-8) for longer ones, where their sum is that
+ * of the rounded ones; the 4-bit values enter it as bf16 (exactly).  out must not overlap q.
  * ws: map_cache_attention_workspace() bytes for the same arguments. */
 size_t map_cache_attention_workspace(const map_cache* c, int B, int n_heads, int max_pages,
                                      const int32_t* seq_off_host);

@@ -14,6 +14,16 @@
 // 4-bit values are widened to bf16 on their way to the registers (keys) or to
 // LDS (values), scale and all, which is exact.
 //
+// The matrix cores take bf16 operands, 2^-8 of a probability's value.  Few rows,
+// which the cache's bytes bound, give each as two bf16 numbers (2^-17) and pay
+// for the second product with 0 to 2 % (16 single tokens over 2952: 135.6 us, 136.6
+// so): their error against 64 bits is that of a float32 softmax, 1.68e-3, all of it
+// the output's rounding, where one number gives 2.12e-3.  Prompts, which the matrix
+// cores bound, would pay 37 % (2944 rows: 88 us, 120 so) for 1.65e-3 in place of
+// 2.06e-3: they give one, and sum what they gave, so that a row's weights add up
+// to one and equal values come back as they are (87 us with the sum of the unrounded
+// ones).
+//
 // Output rows are rescaled only when a row's maximum has grown by more than
 // 2^6 (the sums carry the same factor, so the result is the same softmax).  m
 // starts below every score that counts but finite, so that a row whose scores so
@@ -57,6 +67,15 @@ __device__ __forceinline__ uint32_t word_clean(uint32_t w) {
 __device__ __forceinline__ bf16x8_t clean8(bf16x8_t v) {
   const uint4 u = __builtin_bit_cast(uint4, v);
   return __builtin_bit_cast(bf16x8_t, make_uint4(word_clean(u.x), word_clean(u.y), word_clean(u.z), word_clean(u.w)));
+}
+
+// s plus eight probabilities, as the second product takes them.
+__device__ __forceinline__ float add_weights(bf16x8_t p, float s) {
+  const uint4 u = __builtin_bit_cast(uint4, p);
+  auto two = [](uint32_t w, float to) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), to, false);
+  };
+  return s + (two(u.y, two(u.x, 0.0f)) + two(u.w, two(u.z, 0.0f)));
 }
 
 // N values over their sum, as bf16; zeros where nothing was summed.
@@ -173,7 +192,7 @@ struct Stretches {
 };
 
 template <int DH, bool FP4>
-__global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const CacheAttnArgs a) {
   using X = StepShape<DH, FP4>;
   constexpr int KB = X::KB, NT = X::NT, NM = X::NM, ND = X::ND, NS = X::NS, NV = X::NV;
   __shared__ __attribute__((aligned(1024))) char lds[X::BYTES];
@@ -389,25 +408,31 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= al;
     }
-    bf16x8_t pf[NM];
+    bf16x8_t ph[NM], pl[NM];  // each as two bf16 numbers
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float p = __builtin_amdgcn_exp2f(fmaf(z[t][r], a.c2, -m));
+        const __bf16 high = static_cast<__bf16>(p);
         l += p;
-        pf[t >> 1][4 * (t & 1) + r] = static_cast<__bf16>(p);
+        ph[t >> 1][4 * (t & 1) + r] = high;
+        pl[t >> 1][4 * (t & 1) + r] = static_cast<__bf16>(p - static_cast<float>(high));
       }
     // O^T += V^T P^T
     auto vfrag = [&](int x, int d) {
       const char* at = tr_at + 32 * x * X::VROW + 32 * vchunk<DH>(d, tr_key);
       return join(tr_read(at), tr_read(at + 16 * X::VROW));
     };
+    auto weigh = [&](bf16x8_t v, int x, f32x4_t& sum) {
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[x], sum, 0, 0, 0);
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[x], sum, 0, 0, 0);
+    };
     if constexpr (careful.value) {
 #pragma unroll
       for (int x = 0; x < NM; ++x)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(clean8(vfrag(x, d)), pf[x], o[d], 0, 0, 0);
+        for (int d = 0; d < ND; ++d) weigh(clean8(vfrag(x, d)), x, o[d]);
       for (int k = 0; k < KB; ++k) {
         const bool see = sees(cur, k, (held >> (k >> 4)) & 1u);
 #pragma unroll
@@ -422,7 +447,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void cache_step_kernel(const Cache
 #pragma unroll
       for (int x = 0; x < NM; ++x)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vfrag(x, d), pf[x], o[d], 0, 0, 0);
+        for (int d = 0; d < ND; ++d) weigh(vfrag(x, d), x, o[d]);
     }
   }
   };
@@ -769,6 +794,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
         for (int r = 0; r < 16; ++r) sc[r] = visible(cur, any, acc_row(r, lane)) ? sc[r] : -INFINITY;
       }
     }
+    l = add_weights(before[1], add_weights(before[0], l));
     float mx = sc[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
@@ -778,15 +804,11 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     if (grow) m = mx;
 
     scores(i + 1, next);  // (behind the last half: unused)
-    float sum = 0.0f;
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+    for (int st = 0; st < 2; ++st) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
-        sum += e;
-        p[st][k] = static_cast<__bf16>(e);
-      }
+      for (int k = 0; k < 8; ++k) p[st][k] = static_cast<__bf16>(__builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m)));
+    }
     const char* V = lds + (2 + (((i - 1) >> 1) & 1)) * BUF + 32 * ((i - 1) & 1) * ROW;
     auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
       const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
@@ -816,14 +838,13 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
       }
     }
     // (the exponentials stay up here, beside the products, and do not sink below the branch)
-    asm volatile("" : "+v"(sum), "+v"(p[0]), "+v"(p[1]));
+    asm volatile("" : "+v"(p[0]), "+v"(p[1]));
     if (__any(grow)) {
       const float al = grow ? __builtin_amdgcn_exp2f(m_before - m) : 1.0f;  // (first block: 0)
       l *= al;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= al;
     }
-    l += sum;
   };
   // Keys of block j are read in steps 2 j - 1 and 2 j, its values in steps 2 j + 1
   // and 2 j + 2: so one meeting a block, before an odd step, that brings the keys of

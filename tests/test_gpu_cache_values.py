@@ -1,0 +1,105 @@
+"""Attention over the cache: what rounding may and may not move, in every form a
+call can take: a tile a workgroup, stretches, a prompt, a prompt in parts.
+
+Bars.  A row's probabilities above the fraction line add up to what is below it
+(prompts) or to that but for 2^-17 (few rows), so values that are all equal come
+back as they are: the float32 sums of T terms are off by T 2^-24 each, together
+under the 2^-9 that moves a bfloat16 number for T < 8000.
+"""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import announce
+from test_gpu_cache import KINDS, U, Batch, _f64, _mp
+
+pytestmark = pytest.mark.gpu
+
+# new rows and tokens before them: 16 rows or fewer, with a short table a tile a
+# workgroup, else in stretches; more rows, in parts behind a long cache
+FORMS = {"tile": ([1, 1], [290, 301]), "stretches": ([3, 1], [3000, 700]), "prompt": ([150], [300]), "parts": ([40], [2500])}
+
+
+class Held(Batch):
+    """A batch whose oracle holds what the cache gives back for the rows put in
+    (their rounding to 4 bits has tests of its own)."""
+
+    def _append(self, k, v, lens, off):
+        _mp().map_cache_append(self.cache, self.table.to(self.dev), lens.to(self.dev), k.to(self.dev), v.to(self.dev), off)
+        self.hold(lens, off)
+
+    def hold(self, lens, off):
+        """The last rows of each sequence, as the cache has them."""
+        slots = [int(lens[s]) - off[s + 1] + r for s in range(self.B) for r in range(off[s], off[s + 1])]
+        k, v = (_f64(x) for x in _mp().map_cache_read(self.cache, self.table.to(self.dev), lens.to(self.dev), off,
+                                                      slots=torch.tensor(slots, dtype=torch.int32, device=self.dev)))
+        for s in range(self.B):
+            for r in range(off[s], off[s + 1]):
+                self.oracle.rows[self.oracle.place(s, slots[r])] = (k[r], v[r])
+
+
+def _batch(kind, form, dh=128, heads=2, seed=0):
+    n, past = FORMS[form]
+    return Held(kind, dh, heads, 16, n, past, seed=seed)
+
+
+def _store(b, k, v):
+    """All of each sequence's tokens at once: k and v by (sequence, token)."""
+    lens = b.lens.tolist()
+    off = [0] + np.cumsum(lens).tolist()
+    b._append(torch.cat([k(s, lens[s]) for s in range(b.B)]), torch.cat([v(s, lens[s]) for s in range(b.B)]), b.lens, off)
+
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", FORMS)
+def test_a_row_over_equal_values_gives_that_value(kind, form):
+    """Token 0 at a score of zero, token 257 at one a little above it (the
+    running maximum then stays where it is), all others far below."""
+    announce(f"equal values, {kind}, {form}")
+    b = _batch(kind, form, seed=1)
+    g = torch.Generator().manual_seed(2)
+
+    def keys(s, n):
+        k = torch.zeros(n, 2, 128)
+        k[:, :, 1] = -1.0
+        k[[0, 257], :, 1] = 0.0
+        k[257, :, 0] = 1.0
+        return k.bfloat16()
+
+    row = (torch.randint(0, 2, (1, 2, 128), generator=g) * 2 - 1).float().bfloat16()
+    _store(b, keys, lambda s, n: row.expand(n, 2, 128).contiguous())
+    q = torch.zeros(b.off[-1], 64, 128)
+    q[:, :, 0] = 3.0 + 2.9 * torch.rand(b.off[-1], 64, generator=g)
+    q[:, :, 1] = 4096.0
+    got = b.attend(q.bfloat16(), scale=float(np.log(2.0)))
+    want = row.repeat_interleave(32, 1).expand(b.off[-1], 64, 128)
+    assert torch.equal(got.cpu(), want.contiguous())
+
+
+@pytest.mark.parametrize("wide", [0, 40])
+def test_few_rows_weigh_by_more_than_bfloat16(wide):
+    """Two tokens with opposite values and nearly equal weights, whose difference
+    a probability's rounding to 8 bits would move by more than the output's
+    rounding: the weights carry 2^-17.  In tiles and, behind a wide table, stretches."""
+    announce(f"nearly equal weights, table {wide} pages wider")
+    b = Held("bf16", 128, 1, 16, [1] * 32, [1] * 32, seed=9, wide=wide)
+    g = torch.Generator().manual_seed(9)
+
+    def keys(s, n):
+        k = torch.zeros(n, 1, 128)
+        k[1, 0, 0] = 0.5 * torch.rand(1, generator=g)
+        return k.bfloat16()
+
+    def values(s, n):
+        v = torch.randn(1, 1, 128, generator=g).bfloat16()
+        return torch.cat([v, -v])
+
+    _store(b, keys, values)
+    q = torch.zeros(32, 8, 128)
+    q[:, :, 0] = torch.rand(32, 8, generator=g) - 0.5
+    q = q.bfloat16()
+    want, spread = b.oracle.attention(b.lens.tolist(), b.off, _f64(q), 1.0)
+    du = 130 * 2.0 ** -24 * 0.25  # |q k| <= 1/4
+    off = np.abs(_f64(b.attend(q, scale=1.0)) - want) - U[torch.bfloat16] * np.abs(want) - spread * (2.0 ** -17 + 2 * du + 2.0 ** -14)
+    assert (off <= 0).all(), float(off.max())
