@@ -42,6 +42,12 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
 constexpr float kLow = -3.0e38f;   // m before the first visible score
 constexpr float kRescale = 6.0f;   // log2 of the growth that a row's factor may lag behind
+// Sums of finite values may pass float32's range where their mean does not.  A tile
+// whose sums come out infinite is run again with its probabilities times 2^-40, for
+// up to 2^30 tokens with probabilities up to 2^6; its l is then kept negative, which
+// tells the joins.  They form their sums times their `down`, for as many pieces.  All
+// of these are powers of two: nothing else about a row changes.
+constexpr float kShrink = 0x1p-40f;
 
 // The larger of lanes l and l ^ 32, in both.
 __device__ __forceinline__ float max_of_halves(float x) {
@@ -76,6 +82,12 @@ __device__ __forceinline__ float add_weights(bf16x8_t p, float s) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), to, false);
   };
   return s + (two(u.y, two(u.x, 0.0f)) + two(u.w, two(u.z, 0.0f)));
+}
+
+// What a piece's sums (m, l) count in a join: mm the largest maximum, shrunk whether
+// any piece's l is negative.  (A piece that saw nothing has sums of zero.)
+__device__ __forceinline__ float piece_weight(float m, float l, float mm, bool shrunk, float down) {
+  return __builtin_amdgcn_exp2f(m - mm) * (shrunk & (l >= 0.0f) ? kShrink * down : down);
 }
 
 // N values over their sum, as bf16; zeros where nothing was summed.
@@ -413,7 +425,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(z[t][r], a.c2, -m));
+        float p = __builtin_amdgcn_exp2f(fmaf(z[t][r], a.c2, -m));
+        if constexpr (careful.value) p *= kShrink;
         const __bf16 high = static_cast<__bf16>(p);
         l += p;
         ph[t >> 1][4 * (t & 1) + r] = high;
@@ -451,16 +464,20 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
     }
   }
   };
-  // Every value taken as finite; if a sum comes out infinite or NaN and the tile
-  // has several rows, once more keeping such values from the rows that do not see
-  // them (their zero probability would not cancel them): the product runs on the
+  // Every value taken as finite; if a sum comes out infinite or NaN, once more with
+  // smaller probabilities (kShrink), and keeping such values from the rows that do not
+  // see them (their zero probability would not cancel them): the product runs on the
   // finite values, the others add themselves to the rows that see them.
   run(std::false_type{});
-  if (i_lo != i_hi) {
+  bool shrunk = false;
+  {
     f32x4_t any = {0.0f, 0.0f, 0.0f, 0.0f};  // NaN once a sum is not finite
 #pragma unroll
     for (int d = 0; d < ND; ++d) any += o[d] * 0.0f;
-    if (__any(any[0] + any[1] + any[2] + any[3] != 0.0f)) run(std::true_type{});
+    if (__any(any[0] + any[1] + any[2] + any[3] != 0.0f)) {
+      run(std::true_type{});
+      shrunk = true;
+    }
   }
 
   // join the waves
@@ -468,7 +485,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
   l += __shfl_xor(l, 32, 64);
   if (g4 == 0) {
     ms[wave][lc] = m;
-    ls[wave][lc] = l;
+    ls[wave][lc] = shrunk ? -l : l;
   }
   __syncthreads();  // (V is read out)
   float* os = reinterpret_cast<float*>(lds) + wave * 16 * X::OLD;
@@ -479,15 +496,19 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
   const int c = tid >> 4, d0 = (tid & 15) * PER;
   if (col0 + c < cols) {
     float mm = kLow, sum = 0.0f, v[PER];
+    bool any = false;
 #pragma unroll
-    for (int w = 0; w < kStepWaves; ++w) mm = fmaxf(mm, ms[w][c]);
+    for (int w = 0; w < kStepWaves; ++w) {
+      mm = fmaxf(mm, ms[w][c]);
+      any |= ls[w][c] < 0.0f;
+    }
 #pragma unroll
     for (int k = 0; k < PER; ++k) v[k] = 0.0f;
 #pragma unroll
     for (int w = 0; w < kStepWaves; ++w) {
-      const float lw = ls[w][c], f = __builtin_amdgcn_exp2f(ms[w][c] - mm);
+      const float lw = ls[w][c], f = piece_weight(ms[w][c], lw, mm, any, 0x1p-3f);
       if (lw == 0.0f) continue;
-      sum = fmaf(f, lw, sum);
+      sum = fmaf(f, fabsf(lw), sum);
       const float* src = reinterpret_cast<const float*>(lds) + (w * 16 + c) * X::OLD + d0;
 #pragma unroll
       for (int k = 0; k < PER; ++k) v[k] = fmaf(f, src[k], v[k]);
@@ -497,7 +518,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
       write_row<PER>(static_cast<bf16_t*>(a.out) + (r0 + rr) * a.ldo + hh * DH + d0, v, sum);
     } else {  // the stretch's first tile, or its last
       const long long at = (2LL * blockIdx.x + (x == x_begin ? 0 : 1)) * 16 + c;
-      if (d0 == 0) a.step_ml[at] = make_float2(mm, sum);
+      if (d0 == 0) a.step_ml[at] = make_float2(mm, any ? -sum : sum);
       float4* po = reinterpret_cast<float4*>(a.step_o + at * DH + d0);
 #pragma unroll
       for (int k = 0; k < PER / 4; ++k) po[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
@@ -538,13 +559,19 @@ __global__ __launch_bounds__(256) void cache_step_join_kernel(const CacheAttnArg
   auto piece = [&](int w) {  // the first tile of its stretch, or the last
     return (2LL * w + (first <= all.begin(w) ? 0 : 1)) * 16 + c;
   };
-  for (int w = w0; w <= w1; ++w) mm = fmaxf(mm, a.step_ml[piece(w)].x);
+  float low = 0.0f;  // the least l
+#pragma unroll 8
+  for (int w = w0; w <= w1; ++w) {
+    const float2 ml = a.step_ml[piece(w)];
+    mm = fmaxf(mm, ml.x);
+    low = fminf(low, ml.y);
+  }
 #pragma unroll 4
   for (int w = w0; w <= w1; ++w) {
     const float2 ml = a.step_ml[piece(w)];
-    const float f = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mm);
+    const float f = piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-10f);
     const float4* po = reinterpret_cast<const float4*>(a.step_o + piece(w) * DH + d0);
-    sum = fmaf(f, ml.y, sum);
+    sum = fmaf(f, fabsf(ml.y), sum);
 #pragma unroll
     for (int k = 0; k < PER / 4; ++k) {
       const float4 o = po[k];
@@ -570,14 +597,19 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheAttnA
     if (b + s < a.B && a.off[b + s] <= r) b += s;
   if (a.off[b + 1] - a.off[b] <= a.step_rows) return;  // (written by the few rows' kernel)
   float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float low = 0.0f;  // the least l
 #pragma unroll 8
-  for (int s = 0; s < a.prompt_splits; ++s) mm = fmaxf(mm, a.part_ml[(long long)s * items + item].x);
+  for (int s = 0; s < a.prompt_splits; ++s) {
+    const float2 ml = a.part_ml[(long long)s * items + item];
+    mm = fmaxf(mm, ml.x);
+    low = fminf(low, ml.y);
+  }
 #pragma unroll 8  // (their loads together: no branch on a part that saw nothing, whose sums are zeros)
   for (int s = 0; s < a.prompt_splits; ++s) {
     const float2 ml = a.part_ml[(long long)s * items + item];
-    const float f = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mm);
+    const float f = piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-7f);
     const float4 o = *reinterpret_cast<const float4*>(a.part_o + ((long long)s * items + item) * DH + d0);
-    sum = fmaf(f, ml.y, sum);
+    sum = fmaf(f, fabsf(ml.y), sum);
     v[0] = fmaf(f, o.x, v[0]);
     v[1] = fmaf(f, o.y, v[1]);
     v[2] = fmaf(f, o.z, v[2]);
@@ -807,7 +839,10 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) p[st][k] = static_cast<__bf16>(__builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m)));
+      for (int k = 0; k < 8; ++k) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
+        p[st][k] = static_cast<__bf16>(careful.value ? e * kShrink : e);
+      }
     }
     const char* V = lds + (2 + (((i - 1) >> 1) & 1)) * BUF + 32 * ((i - 1) & 1) * ROW;
     auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
@@ -850,9 +885,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   // and 2 j + 2: so one meeting a block, before an odd step, that brings the keys of
   // the block after next and the values of the next.
   // A first run takes every value as finite; if a sum comes out infinite or NaN, a
-  // second one keeps such values from the rows that do not see them (their zero
-  // probability would not cancel them): the product runs on the finite values, and
-  // the others add themselves to the rows that see them.
+  // second one has smaller probabilities (kShrink) and keeps such values from the rows
+  // that do not see them (their zero probability would not cancel them): the product
+  // runs on the finite values, and the others add themselves to the rows that see them.
   auto run = [&](auto careful) {
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -909,14 +944,15 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing on its way to LDS
     return __syncthreads_or(any != 0.0f && q0 + 32 * wave + lr < n);  // (and K and V are read out)
   };
-  if (run(std::false_type{})) run(std::true_type{});
+  const bool shrunk = run(std::false_type{});
+  if (shrunk) run(std::true_type{});
   if (whi <= wlo) return;
   l += __shfl_xor(l, 32, 64);
   const int i = q0 + 32 * wave + lr;  // this lane's row
   if (a.prompt_splits > 1) {
     if (i >= n) return;
     const long long at = ((long long)part * a.off[a.B] + r0 + i) * a.Hq + h;
-    if (lh == 0) a.part_ml[at] = make_float2(m, l);
+    if (lh == 0) a.part_ml[at] = make_float2(m, shrunk ? -l : l);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll

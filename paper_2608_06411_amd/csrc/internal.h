@@ -481,9 +481,9 @@ struct CacheAttnArgs {
   int tiles, step_rows, groups, prompt_splits;
   int32_t* step_run;      // [2 B + 1] each sequence's first block and its length; all blocks
   float* step_o;          // [groups][2][16][Dh] sums of a stretch's first and last tile, with stretches
-  float2* step_ml;        // [groups][2][16] and (m, l)
+  float2* step_ml;        // [groups][2][16] and (m, l); l negative: sums of smaller probabilities
   float* part_o;          // [part][rows][Hq][Dh] each part's sums, where there are several
-  float2* part_ml;        // [part][rows][Hq] and (m, l)
+  float2* part_ml;        // [part][rows][Hq] and (m, l), likewise
   int off[MAP_CACHE_MAX_BATCH + 1];
 };
 // How a call is divided (the workspace holds what is joined later), and the call.

@@ -1,4 +1,4 @@
-"""Attention over the cache: what rounding may and may not move, in every form a
+"""Attention over the cache: what rounding and range may and may not move, in every form a
 call can take: a tile a workgroup, stretches, a prompt, a prompt in parts.
 
 Bars.  A row's probabilities above the fraction line add up to what is below it
@@ -103,3 +103,54 @@ def test_few_rows_weigh_by_more_than_bfloat16(wide):
     du = 130 * 2.0 ** -24 * 0.25  # |q k| <= 1/4
     off = np.abs(_f64(b.attend(q, scale=1.0)) - want) - U[torch.bfloat16] * np.abs(want) - spread * (2.0 ** -17 + 2 * du + 2.0 ** -14)
     assert (off <= 0).all(), float(off.max())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("first", [64, 1 << 30])
+def test_values_whose_sum_passes_float32(kind, form, first):
+    """Values at the end of their range, of one sign a channel: their sum is
+    infinite in float32, their mean is not.  In all tokens, or in the first ones
+    only, so that some waves' and some parts' sums are finite."""
+    announce(f"large values, {kind}, {form}, the first {first}")
+    b = _batch(kind, form, seed=3)
+    g = torch.Generator().manual_seed(4)
+    sign = (torch.randint(0, 2, (1, 2, 128), generator=g) * 2 - 1).double()
+
+    def values(s, n):
+        v = (1.2e38 + 2.1e38 * torch.rand(n, 2, 128, generator=g).double()) * sign
+        v[first:] = torch.randn(max(n - first, 0), 2, 128, generator=g).double()
+        return v.bfloat16()
+
+    _store(b, lambda s, n: b.rows(n), values)
+    q = b.rows(b.off[-1], heads=4)
+    got = b.attend(q)
+    assert torch.isfinite(got).all()
+    b.check(q, got=got)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", FORMS)
+def test_large_values_beside_hidden_ones(kind, form):
+    """... and a NaN in the last row's own token, which the other rows do not see."""
+    announce(f"large values beside a hidden NaN, {kind}, {form}")
+    b = _batch(kind, form, seed=5)
+    g = torch.Generator().manual_seed(6)
+
+    def values(s, n):
+        v = (1.2e38 + 2.1e38 * torch.rand(n, 2, 128, generator=g).double()).bfloat16()
+        if s == 0:
+            v[n - 1, :, 5] = float("nan")
+        return v
+
+    _store(b, lambda s, n: b.rows(n), values)
+    q = b.rows(b.off[-1], heads=4)
+    last = b.n[0] - 1
+    got = b.attend(q)
+    assert torch.isnan(got[last, :, 5]).all()
+    keep = [r for r in range(b.off[-1]) if r != last]
+    assert torch.isfinite(got[keep]).all()
+    want, spread = b.oracle.attention(b.lens.tolist(), b.off, _f64(q), 128 ** -0.5)
+    du = 130 * 2.0 ** -24 * 128 ** -0.5 * np.abs(_f64(q)).sum(-1).max() * max(np.abs(r[0]).max() for r in b.oracle.rows.values())
+    bar = U[torch.bfloat16] * (np.abs(want) + spread) + spread * (2 * du + 2.0 ** -14)
+    assert (np.abs(_f64(got) - want) <= bar)[keep].all()
