@@ -455,7 +455,7 @@ map_status map_cache_read(const map_cache* c, map_dtype dt, int B, const int32_t
  * token i sees the tokens j <= i with i - j < window or j < sinks (window = 0:
  * all of them).  A row that sees nothing gives zeros, and what a row does not
  * see adds nothing to it, whatever it holds (NaN, infinities).  A score below
- * -3e38 weighs nothing.
+ * -3e38 weighs nothing; a row that sees one past 3.4e38 is NaN.
  * q [rows][n_heads][head_dim] bf16, rows ldq apart; out likewise, ldo apart;
  * n_heads a multiple of n_kv_heads, at most 1024; 0 < scale < 1e30.  Scores, the softmax and its
  * sums are float32; probabilities enter the second product as two bf16 numbers each (2^-17 of their

@@ -75,6 +75,17 @@ __device__ __forceinline__ bf16x8_t clean8(bf16x8_t v) {
   return __builtin_bit_cast(bf16x8_t, make_uint4(word_clean(u.x), word_clean(u.y), word_clean(u.z), word_clean(u.w)));
 }
 
+// The exponent of a probability is one multiply-add of a score, which rounds once; m
+// was rounded before it.  At scores past 2^26 the two differ by more than the exponents
+// of the type: the largest probability is no longer about one.  Such a row shows in
+// its l; its tile is run again, with the row's products rounded as m's was.
+__device__ __forceinline__ bool far_scores(float m, float l) { return (m > kLow) & !((l >= 0.25f) & (l < INFINITY)); }
+__device__ __forceinline__ float exponent_apart(float score, float c2, float m) {
+#pragma clang fp contract(off)
+  const float x = score * c2;
+  return x - m;
+}
+
 // s plus eight probabilities, as the second product takes them.
 __device__ __forceinline__ float add_weights(bf16x8_t p, float s) {
   const uint4 u = __builtin_bit_cast(uint4, p);
@@ -87,7 +98,7 @@ __device__ __forceinline__ float add_weights(bf16x8_t p, float s) {
 // What a piece's sums (m, l) count in a join: mm the largest maximum, shrunk whether
 // any piece's l is negative.  (A piece that saw nothing has sums of zero.)
 __device__ __forceinline__ float piece_weight(float m, float l, float mm, bool shrunk, float down) {
-  return __builtin_amdgcn_exp2f(m - mm) * (shrunk & (l >= 0.0f) ? kShrink * down : down);
+  return __builtin_amdgcn_exp2f(m - mm) * ((shrunk & (l >= 0.0f)) ? kShrink * down : down);
 }
 
 // N values over their sum, as bf16; zeros where nothing was summed.
@@ -329,6 +340,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
     const int tok = cur + k;
     return static_cast<bool>((page != 0u) & (tok <= me) & ((tok >= from) | (tok < a.sinks)));
   };
+  bool apart = false;  // this row's scores are far
   auto run = [&](auto careful) {
   m = kLow;
   l = 0.0f;
@@ -426,7 +438,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float p = __builtin_amdgcn_exp2f(fmaf(z[t][r], a.c2, -m));
-        if constexpr (careful.value) p *= kShrink;
+        if constexpr (careful.value) p = kShrink * (apart ? __builtin_amdgcn_exp2f(exponent_apart(z[t][r], a.c2, m)) : p);
         const __bf16 high = static_cast<__bf16>(p);
         l += p;
         ph[t >> 1][4 * (t & 1) + r] = high;
@@ -464,25 +476,31 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
     }
   }
   };
-  // Every value taken as finite; if a sum comes out infinite or NaN, once more with
-  // smaller probabilities (kShrink), and keeping such values from the rows that do not
-  // see them (their zero probability would not cancel them): the product runs on the
-  // finite values, the others add themselves to the rows that see them.
+  // Every value taken as finite; if a sum comes out infinite or NaN (or a score is far:
+  // far_scores), once more with
+  // smaller probabilities (kShrink), and keeping such values from the rows that
+  // do not see them (their zero probability would not cancel them): the product runs on
+  // the finite values, the others add themselves to the rows that see them.
   run(std::false_type{});
+  auto sum_l = [&]() {
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+  };
+  sum_l();
   bool shrunk = false;
   {
+    apart = far_scores(m, l);
     f32x4_t any = {0.0f, 0.0f, 0.0f, 0.0f};  // NaN once a sum is not finite
 #pragma unroll
     for (int d = 0; d < ND; ++d) any += o[d] * 0.0f;
-    if (__any(any[0] + any[1] + any[2] + any[3] != 0.0f)) {
+    if (__any(apart | (any[0] + any[1] + any[2] + any[3] != 0.0f))) {
       run(std::true_type{});
+      sum_l();
       shrunk = true;
     }
   }
 
   // join the waves
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
   if (g4 == 0) {
     ms[wave][lc] = m;
     ls[wave][lc] = shrunk ? -l : l;
@@ -793,6 +811,7 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   f32x16_t o[ND];  // O^T: rows 32 d + acc_row = values, column lr = the query
   float m, l;
   const float c2 = a.c2;
+  bool apart = false;  // this row's scores are far
   const int tr_key = 4 * lh + ((lane & 15) >> 2);
   auto token_of = [&](int i) { return blocks.token(i >> 1, kKeys) + 32 * (i & 1); };
   // S^T of half i: rows = keys acc_row, column = the query
@@ -840,8 +859,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     for (int st = 0; st < 2; ++st) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
-        p[st][k] = static_cast<__bf16>(careful.value ? e * kShrink : e);
+        float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
+        if constexpr (careful.value) e = kShrink * (apart ? __builtin_amdgcn_exp2f(exponent_apart(sc[8 * st + k], c2, m)) : e);
+        p[st][k] = static_cast<__bf16>(e);
       }
     }
     const char* V = lds + (2 + (((i - 1) >> 1) & 1)) * BUF + 32 * ((i - 1) & 1) * ROW;
@@ -884,7 +904,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   // Keys of block j are read in steps 2 j - 1 and 2 j, its values in steps 2 j + 1
   // and 2 j + 2: so one meeting a block, before an odd step, that brings the keys of
   // the block after next and the values of the next.
-  // A first run takes every value as finite; if a sum comes out infinite or NaN, a
+  // A first run takes every value as finite; if a sum comes out infinite or NaN, or a score
+  // is far (far_scores), a
   // second one has smaller probabilities (kShrink) and keeps such values from the rows
   // that do not see them (their zero probability would not cancel them): the product
   // runs on the finite values, and the others add themselves to the rows that see them.
@@ -941,8 +962,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) any = fmaf(o[d][r], 0.0f, any);
+    apart = far_scores(m, l + __shfl_xor(l, 32, 64));
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing on its way to LDS
-    return __syncthreads_or(any != 0.0f && q0 + 32 * wave + lr < n);  // (and K and V are read out)
+    return __syncthreads_or((apart | (any != 0.0f)) & (q0 + 32 * wave + lr < n));  // (and K and V are read out)
   };
   const bool shrunk = run(std::false_type{});
   if (shrunk) run(std::true_type{});

@@ -4,7 +4,10 @@ call can take: a tile a workgroup, stretches, a prompt, a prompt in parts.
 Bars.  A row's probabilities above the fraction line add up to what is below it
 (prompts) or to that but for 2^-17 (few rows), so values that are all equal come
 back as they are: the float32 sums of T terms are off by T 2^-24 each, together
-under the 2^-9 that moves a bfloat16 number for T < 8000.
+under the 2^-9 that moves a bfloat16 number for T < 8000.  Elsewhere, with u = 2^-8
+and spread = sum p |v|, a probability's rounding and the output's: u (|o| + spread)
++ spread 2^-14 for the exponentials and the sums; the far scores are single
+products, exact in float32.
 """
 import numpy as np
 import pytest
@@ -49,6 +52,11 @@ def _store(b, k, v):
     off = [0] + np.cumsum(lens).tolist()
     b._append(torch.cat([k(s, lens[s]) for s in range(b.B)]), torch.cat([v(s, lens[s]) for s in range(b.B)]), b.lens, off)
 
+
+def _near(got, want, spread):
+    bar = U[torch.bfloat16] * (np.abs(want) + spread) + spread * 2.0 ** -14
+    off = np.abs(got - want) - bar
+    assert (off <= 0).all(), (np.argwhere(~(off <= 0))[:4].tolist(), float(np.abs(got).max()))
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -154,3 +162,28 @@ def test_large_values_beside_hidden_ones(kind, form):
     du = 130 * 2.0 ** -24 * 128 ** -0.5 * np.abs(_f64(q)).sum(-1).max() * max(np.abs(r[0]).max() for r in b.oracle.rows.values())
     bar = U[torch.bfloat16] * (np.abs(want) + spread) + spread * (2 * du + 2.0 ** -14)
     assert (np.abs(_f64(got) - want) <= bar)[keep].all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("far", [20, 27, 31, 36, 60])
+def test_far_scores(kind, form, far):
+    """Scores of plus and minus 1.77 times 2^far: half of the tokens share each
+    row's weight, whatever their score times log2(e) rounds to."""
+    announce(f"scores of 2^{far}, {kind}, {form}")
+    b = _batch(kind, form, seed=far)
+    g = torch.Generator().manual_seed(far)
+
+    def keys(s, n):
+        k = torch.zeros(n, 2, 128)
+        k[:, :, 0] = (torch.randint(0, 2, (n, 2), generator=g) * 2 - 1) * 1.5 * 2.0 ** (far // 2)
+        return k.bfloat16()
+
+    _store(b, keys, lambda s, n: b.rows(n))
+    q = torch.zeros(b.off[-1], 4, 128)
+    q[:, :, 0] = 151 / 128 * 2.0 ** (far - far // 2)
+    q[::2, 1, 0] *= -1.0
+    q = q.bfloat16()
+    for scale in (1.0, 0.7):
+        want, spread = b.oracle.attention(b.lens.tolist(), b.off, _f64(q), float(np.float32(scale)))
+        _near(_f64(b.attend(q, scale=scale)), want, spread)
