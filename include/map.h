@@ -389,7 +389,8 @@ typedef struct {
  * the same stride); otherwise inputs and outputs must not overlap.
  * pos [n_axes][ldpos] int32, row r's position on axis a at a ldpos + r.
  * dt: MAP_F32 or MAP_BF16 for q, k, the norms and the outputs; sums and the
- * rotation are float32, angles float64.  1 <= heads <= 1024 each; R = 0 does
+ * rotation are float32 (a head whose sum of squares would pass its range is summed
+ * times a power of two), angles float64.  1 <= heads <= 1024 each; R = 0 does
  * nothing. */
 map_status map_qk_norm_rope(const map_rope* rp, map_dtype dt, int R, int n_heads, int n_kv_heads,
                             const void* q, int64_t ldq, const void* k, int64_t ldk,

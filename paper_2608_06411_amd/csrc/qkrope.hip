@@ -88,7 +88,24 @@ __global__ __launch_bounds__(NT) void qk_norm_rope_kernel(const QkRopeArgs a) {
 #pragma unroll
     for (int off = LPH / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off, 64);
     if (g) {
-      const float inv = 1.0f / sqrtf(ss / static_cast<float>(DH) + a.eps);
+      // A sum of squares past float32's range, or under it where eps does not hide
+      // that: once more, the head times a power of two.
+      float eps = a.eps;
+      const bool far = !(ss < 3e38f) | ((ss < 1e-30f) & (eps < 1e-36f));
+      if (__any(far)) {
+        const float t = far ? (ss < 1.0f ? 0x1p100f : 0x1p-70f) : 1.0f;
+        eps = eps * t * t;
+        ss = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] *= t;
+          y[k] *= t;
+          ss = fmaf(x[k], x[k], fmaf(y[k], y[k], ss));
+        }
+#pragma unroll
+        for (int off = LPH / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off, 64);
+      }
+      const float inv = 1.0f / sqrtf(ss / static_cast<float>(DH) + eps);
       Piece<T> gu, gv;
       gu.load(g + i0);
       gv.load(g + i1);

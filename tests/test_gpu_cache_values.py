@@ -1,5 +1,6 @@
-"""Attention over the cache: what rounding and range may and may not move, in every form a
-call can take: a tile a workgroup, stretches, a prompt, a prompt in parts.
+"""Attention over the cache and the head norms: what rounding and range may and may
+not move; attention in every form a call can take: a tile a workgroup, stretches, a
+prompt, a prompt in parts.
 
 Bars.  A row's probabilities above the fraction line add up to what is below it
 (prompts) or to that but for 2^-17 (few rows), so values that are all equal come
@@ -13,7 +14,8 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_util import announce
+import oracle.cache as oc
+from gpu_util import announce, device
 from test_gpu_cache import KINDS, U, Batch, _f64, _mp
 
 pytestmark = pytest.mark.gpu
@@ -187,3 +189,47 @@ def test_far_scores(kind, form, far):
     for scale in (1.0, 0.7):
         want, spread = b.oracle.attention(b.lens.tolist(), b.off, _f64(q), float(np.float32(scale)))
         _near(_f64(b.attend(q, scale=scale)), want, spread)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size,eps", [(1e-30, 0.0), (1e-22, 1e-38), (1e18, 1e-6), (3e25, 1e-6), (1e38, 0.0)])
+def test_norms_whose_squares_pass_float32(dtype, size, eps):
+    """Heads whose sum of squares is infinite or zero in float32, among ordinary
+    ones; their norms are neither."""
+    mp, dev = _mp(), device()
+    announce(f"norms of heads of {size}, eps {eps}, {dtype}")
+    g = torch.Generator().manual_seed(7)
+    R, Hq, Hk, dh, rot = 9, 10, 3, 128, 64
+    q, k = torch.randn(R, Hq, dh, generator=g).double(), torch.randn(R, Hk, dh, generator=g).double()
+    q[::2, 1::3] *= size / 3
+    k[1::2] *= size / 3
+    q, k = q.to(dtype).to(dev), k.to(dtype).to(dev)
+    pos = torch.randint(0, 5000, (1, R), generator=g, dtype=torch.int32).to(dev)
+    qn, kn = ((1 + 0.2 * torch.randn(2, dh, generator=g)).to(dtype).to(dev)).unbind(0)
+    got = mp.map_qk_norm_rope(mp.RopeParams(dh, rot_dim=rot, eps=eps), q, k, pos, qn, kn)
+    eps = float(np.float32(eps))
+    for x, w, y in ((q, qn, got[0]), (k, kn, got[1])):
+        want = oc.qk_norm_rope(_f64(x), _f64(pos), _f64(w), rot, [rot // 2], eps=eps)
+        a = np.abs(oc.qk_norm_rope(_f64(x), 0 * _f64(pos), _f64(w), rot, [rot // 2], eps=eps))
+        mag = a.copy()
+        mag[..., :rot] = np.tile(a[..., :rot // 2] + a[..., rot // 2:rot], 2)
+        assert (np.abs(_f64(y) - want) <= U[dtype] * np.abs(want) + 32 * 2.0 ** -24 * mag).all()
+
+
+def test_norms_of_zero_and_of_what_is_not_finite():
+    """A head of zeros stays zero; one that holds an infinity or a NaN is the
+    formula's, and its neighbours are what they are without it."""
+    mp, dev = _mp(), device()
+    announce("norms of zeros and infinities")
+    x = torch.randn(4, 6, 64, generator=torch.Generator().manual_seed(8)).to(dev)
+    w, pos, rp = torch.ones(64, device=dev), torch.arange(4, dtype=torch.int32, device=dev), mp.RopeParams(64)
+    clean, _ = mp.map_qk_norm_rope(rp, x, x, pos, w, w)
+    y = x.clone()
+    y[0, 1] = 0.0
+    y[2, 3, 7], y[3, 0, 5] = float("inf"), float("nan")
+    got, _ = mp.map_qk_norm_rope(rp, y, y, pos, w, w)
+    assert not got[0, 1].any() and torch.isnan(got[3, 0]).all()
+    assert torch.isnan(got[2, 3, [7, 39]]).all() and not got[2, 3, [0, 6, 8, 31, 38, 40, 63]].any()
+    same = torch.ones(4, 6, dtype=torch.bool)
+    same[0, 1] = same[2, 3] = same[3, 0] = False
+    assert torch.equal(got[same], clean[same])
