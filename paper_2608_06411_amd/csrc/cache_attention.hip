@@ -605,33 +605,38 @@ __global__ __launch_bounds__(256) void cache_step_join_kernel(const CacheAttnArg
 
 // Joins the parts of the prompts' rows in the same way.
 template <int DH>
-__global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheAttnArgs a) {
+__global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheJoinArgs a) {
   constexpr int LPH = DH / 4;  // lanes a row and head
-  const long long item = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH, items = (long long)a.off[a.B] * a.Hq;
+  const long long item = (long long)blockIdx.x * (256 / LPH) + threadIdx.x / LPH, items = (long long)a.rows * a.Hq;
   if (item >= items) return;
-  const int r = static_cast<int>(item / a.Hq), h = static_cast<int>(item - (long long)r * a.Hq), d0 = 4 * (threadIdx.x % LPH);
-  int b = 0;  // the row's sequence: the last that starts at or before it
+  const int i = static_cast<int>(item / a.Hq), h = static_cast<int>(item - (long long)i * a.Hq), d0 = 4 * (threadIdx.x % LPH);
+  int b = 0;  // the row's prompt: the last that starts at or before it
   for (int s = MAP_CACHE_MAX_BATCH / 2; s > 0; s >>= 1)
-    if (b + s < a.B && a.off[b + s] <= r) b += s;
-  if (a.off[b + 1] - a.off[b] <= a.step_rows) return;  // (written by the few rows' kernel)
-  float mm = kLow, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  float low = 0.0f;  // the least l
-#pragma unroll 8
-  for (int s = 0; s < a.prompt_splits; ++s) {
-    const float2 ml = a.part_ml[(long long)s * items + item];
-    mm = fmaxf(mm, ml.x);
-    low = fminf(low, ml.y);
+    if (b + s < a.prompts && a.prompt[b + s].x <= i) b += s;
+  const int r = a.prompt[b].y + i - a.prompt[b].x;
+  float mm = kLow, low = 0.0f, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // low: the least l
+  // (a few parts' loads together; past the last, that one's again, at no weight)
+  for (int s0 = 0; s0 < a.parts; s0 += 2) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float2 ml = a.part_ml[(long long)min(s0 + u, a.parts - 1) * items + item];
+      mm = fmaxf(mm, ml.x);
+      low = fminf(low, ml.y);
+    }
   }
-#pragma unroll 8  // (their loads together: no branch on a part that saw nothing, whose sums are zeros)
-  for (int s = 0; s < a.prompt_splits; ++s) {
-    const float2 ml = a.part_ml[(long long)s * items + item];
-    const float f = piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-7f);
-    const float4 o = *reinterpret_cast<const float4*>(a.part_o + ((long long)s * items + item) * DH + d0);
-    sum = fmaf(f, fabsf(ml.y), sum);
-    v[0] = fmaf(f, o.x, v[0]);
-    v[1] = fmaf(f, o.y, v[1]);
-    v[2] = fmaf(f, o.z, v[2]);
-    v[3] = fmaf(f, o.w, v[3]);
+  for (int s0 = 0; s0 < a.parts; s0 += 4) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const long long at = (long long)min(s0 + u, a.parts - 1) * items + item;
+      const float2 ml = a.part_ml[at];
+      const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * DH + d0);
+      const float f = s0 + u < a.parts ? piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-7f) : 0.0f;
+      sum = fmaf(f, fabsf(ml.y), sum);
+      v[0] = fmaf(f, o.x, v[0]);
+      v[1] = fmaf(f, o.y, v[1]);
+      v[2] = fmaf(f, o.z, v[2]);
+      v[3] = fmaf(f, o.w, v[3]);
+    }
   }
   write_row<4>(static_cast<bf16_t*>(a.out) + r * a.ldo + h * DH + d0, v, sum);
 }
@@ -972,8 +977,19 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   l += __shfl_xor(l, 32, 64);
   const int i = q0 + 32 * wave + lr;  // this lane's row
   if (a.prompt_splits > 1) {
+    int before = 0, all = 0;  // rows of the prompts before this one, and of all
+    for (int c = lane; c < a.B; c += 64) {
+      const int rows = a.off[c + 1] - a.off[c], of = rows > a.step_rows ? rows : 0;
+      before += c < b ? of : 0;
+      all += of;
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      before += __shfl_xor(before, x, 64);
+      all += __shfl_xor(all, x, 64);
+    }
     if (i >= n) return;
-    const long long at = ((long long)part * a.off[a.B] + r0 + i) * a.Hq + h;
+    const long long at = ((long long)part * all + before + i) * a.Hq + h;
     if (lh == 0) a.part_ml[at] = make_float2(m, shrunk ? -l : l);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -1038,6 +1054,7 @@ CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int D
       step_tiles += (long long)((n * G + 15) / 16) * Hkv;
     } else {
       p.prompt_most = max(p.prompt_most, n);
+      p.prompt_rows += n;
       prompt_tiles += (long long)((n + 127) / 128) * Hq;
     }
   }
@@ -1087,10 +1104,17 @@ hipError_t launch_cache_attention(CacheAttnArgs& a, const CacheAttnPlan& p, hipS
       e = a.Dh == 128 ? launch_kernel("cache_prompt", cache_prompt_kernel<128, false>, grid, block, 0, s, a)
                       : launch_kernel("cache_prompt", cache_prompt_kernel<64, false>, grid, block, 0, s, a);
     if (e == hipSuccess && p.prompt_splits > 1) {
-      const long long items = (long long)a.off[a.B] * a.Hq, per = 256 / (a.Dh / 4);
+      CacheJoinArgs j{a.out, a.ldo, a.part_o, a.part_ml, a.Hq, p.prompt_splits, 0, 0, {}};
+      for (int b = 0; b < a.B; ++b) {
+        const int n = a.off[b + 1] - a.off[b];
+        if (n <= kStepRows) continue;
+        j.prompt[j.prompts++] = make_int2(j.rows, a.off[b]);
+        j.rows += n;
+      }
+      const long long items = (long long)j.rows * a.Hq, per = 256 / (a.Dh / 4);
       const dim3 joins(static_cast<unsigned>((items + per - 1) / per));
-      e = a.Dh == 128 ? launch_kernel("cache_prompt_join", cache_prompt_join_kernel<128>, joins, block, 0, s, a)
-                      : launch_kernel("cache_prompt_join", cache_prompt_join_kernel<64>, joins, block, 0, s, a);
+      e = a.Dh == 128 ? launch_kernel("cache_prompt_join", cache_prompt_join_kernel<128>, joins, block, 0, s, j)
+                      : launch_kernel("cache_prompt_join", cache_prompt_join_kernel<64>, joins, block, 0, s, j);
     }
   }
   return e;

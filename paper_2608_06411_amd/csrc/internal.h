@@ -482,13 +482,23 @@ struct CacheAttnArgs {
   int32_t* step_run;      // [2 B + 1] each sequence's first block and its length; all blocks
   float* step_o;          // [groups][2][16][Dh] sums of a stretch's first and last tile, with stretches
   float2* step_ml;        // [groups][2][16] and (m, l); l negative: sums of smaller probabilities
-  float* part_o;          // [part][rows][Hq][Dh] each part's sums, where there are several
-  float2* part_ml;        // [part][rows][Hq] and (m, l), likewise
+  float* part_o;          // [part][prompt rows][Hq][Dh] each part's sums, where there are several
+  float2* part_ml;        // [part][prompt rows][Hq] and (m, l), likewise
   int off[MAP_CACHE_MAX_BATCH + 1];
+};
+// The join of the prompts' parts.
+struct CacheJoinArgs {
+  void* out;
+  long long ldo;
+  const float* part_o;
+  const float2* part_ml;
+  int Hq, parts, rows, prompts;
+  int2 prompt[MAP_CACHE_MAX_BATCH];  // its first row among the rows of prompts, and among all rows
 };
 // How a call is divided (the workspace holds what is joined later), and the call.
 struct CacheAttnPlan {
   int step_most, prompt_most;  // the longest few-row sequence, the longest prompt (0: none)
+  int prompt_rows;             // of all prompts
   int tiles, groups, prompt_splits;
   bool run_fits;  // the stretches' blocks can be counted: without it a workgroup takes a tile
 };

@@ -1566,7 +1566,7 @@ CacheAttentionWs carve_cache_attention(Carver& w, const map_cache& c, int B, int
   t.plan = cache_attention_plan(off, B, n_heads, c.n_kv_heads, c.head_dim, c.type == MAP_CACHE_MXFP4,
                                 (long long)max_pages * c.page, device_cus());
   const size_t pieces = (size_t)t.plan.groups * 2 * 16;
-  const size_t items = t.plan.prompt_splits > 1 ? (size_t)t.plan.prompt_splits * off[B] * n_heads : 0;
+  const size_t items = t.plan.prompt_splits > 1 ? (size_t)t.plan.prompt_splits * t.plan.prompt_rows * n_heads : 0;
   t.step_run = w.take<int32_t>(2 * MAP_CACHE_MAX_BATCH + 1);
   t.step_ml = w.take<float2>(pieces);
   t.step_o = w.take<float>(pieces * c.head_dim);

@@ -185,3 +185,18 @@ def test_binding_refuses_sizes_past_an_int(bad):
     d = _cpu("bf16")
     with pytest.raises(ValueError, match="31 bits"):
         mp.map_cache_attention(d["cache"], d["table"], d["lens"], d["q"], d["off"], **bad)
+
+
+@pytest.mark.parametrize("few", [1, 16])
+@pytest.mark.parametrize("prompts", [[17], [40, 100]])
+def test_attention_workspace_holds_the_prompts_rows_alone(few, prompts):
+    # The parts of divided prompts are for the prompts' rows: sequences of few rows beside them need no room there.
+    def size(n):
+        off = [0]
+        for x in n:
+            off.append(off[-1] + x)
+        return bd.lib().map_cache_attention_workspace(ctypes.byref(_cache(n_kv_heads=8, page=64)), len(n), 32, 512, _off(*off))
+
+    alone, beside = size(prompts), size([few] * 100 + prompts[:1] + [few] * 150 + prompts[1:])
+    assert alone > 1 << 20
+    assert beside <= alone + size([few] * 250)
