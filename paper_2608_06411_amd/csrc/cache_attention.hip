@@ -616,7 +616,7 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheJoinA
   const int r = a.prompt[b].y + i - a.prompt[b].x;
   float mm = kLow, low = 0.0f, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // low: the least l
   // (a few parts' loads together; past the last, that one's again, at no weight)
-  for (int s0 = 0; s0 < a.parts; s0 += 2) {
+  for (int s0 = 0; s0 < a.parts; s0 += 4) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float2 ml = a.part_ml[(long long)min(s0 + u, a.parts - 1) * items + item];
@@ -624,7 +624,7 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheJoinA
       low = fminf(low, ml.y);
     }
   }
-  for (int s0 = 0; s0 < a.parts; s0 += 4) {
+  for (int s0 = 0; s0 < a.parts; s0 += 2) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const long long at = (long long)min(s0 + u, a.parts - 1) * items + item;
