@@ -849,7 +849,13 @@ def map_cache_read(cache: KVCache, table: torch.Tensor, lens: torch.Tensor, seq_
 def cache_attention_workspace(cache: KVCache, seq_off, n_heads: int, table: torch.Tensor) -> torch.Tensor:
     """A reusable workspace for map_cache_attention over these rows, heads and table."""
     off = _seq(seq_off)
-    nbytes = lib().map_cache_attention_workspace(cache._ref, off.B, n_heads, _dims(table, "table", 2)[1], off._arr)
+    size = lib().map_cache_attention_workspace
+    args = (cache._ref, off.B, n_heads, _dims(table, "table", 2)[1], off._arr)
+    if cache.device.type == "cuda" and cache.device.index != torch.cuda.current_device():
+        with torch.cuda.device(cache.device):  # (a call is divided by its own device's compute units)
+            nbytes = size(*args)
+    else:
+        nbytes = size(*args)
     if nbytes == 0:
         raise MapError(MAP_ERR_INVALID_ARG, "map_cache_attention_workspace")
     return _workspace(nbytes, cache.device)

@@ -200,3 +200,35 @@ def test_attention_workspace_holds_the_prompts_rows_alone(few, prompts):
     alone, beside = size(prompts), size([few] * 100 + prompts[:1] + [few] * 150 + prompts[1:])
     assert alone > 1 << 20
     assert beside <= alone + size([few] * 250)
+
+
+@pytest.mark.parametrize("of,current", [("cuda:1", 0), ("cuda:0", 0), ("cuda:2", 1), ("cpu", 0)])
+def test_attention_workspace_is_sized_on_the_caches_device(monkeypatch, of, current):
+    # The division, and with it the size, follows the current device's compute units: it has to be the cache's.
+    seen, now = [], [current]
+
+    class Guard:
+        def __init__(self, device):
+            self.to = torch.device(device).index
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.to
+
+        def __exit__(self, *_):
+            now[0] = self.was
+
+    class Lib:
+        @staticmethod
+        def map_cache_attention_workspace(*_):
+            seen.append(now[0])
+            return 512
+
+    cache = _cpu()["cache"]
+    cache.device = torch.device(of)
+    monkeypatch.setattr(bd, "lib", lambda: Lib)
+    monkeypatch.setattr(bd, "_workspace", lambda nbytes, device: (nbytes, device))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    got = mp.cache_attention_workspace(cache, [0, 2, 5], 8, torch.zeros(2, 3, dtype=torch.int32))
+    assert got == (512, cache.device) and now == [current]
+    assert seen == [current if of == "cpu" else cache.device.index]
