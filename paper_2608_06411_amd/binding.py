@@ -684,6 +684,8 @@ class KVCache:
     def _set(self, k, v, k_scale, v_scale):
         n_pages, heads, page, width = _dims(k, "k", 4)
         mx = k_scale is not None
+        if mx != (v_scale is not None):
+            raise ValueError("k_scale and v_scale: both (4 bits) or neither (bf16)")
         dh = 2 * width if mx else width
         if page not in (16, 32, 64, 128) or dh not in (64, 128) or not 1 <= heads <= 256 or n_pages < 1:
             raise ValueError(f"a cache has at least one page, of 16, 32, 64 or 128 tokens, 1 to 256 heads and a head_dim "

@@ -232,3 +232,13 @@ def test_attention_workspace_is_sized_on_the_caches_device(monkeypatch, of, curr
     got = mp.cache_attention_workspace(cache, [0, 2, 5], 8, torch.zeros(2, 3, dtype=torch.int32))
     assert got == (512, cache.device) and now == [current]
     assert seen == [current if of == "cpu" else cache.device.index]
+
+
+@pytest.mark.parametrize("missing", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("kind", ["bf16", "mxfp4"])
+def test_from_tensors_refuses_one_scale(kind, missing):
+    c, s = mp.KVCache(2, 16, 1, 64, kind, device="cpu"), torch.zeros(2, 1, 16, 2, dtype=torch.uint8)
+    with pytest.raises((ValueError, TypeError), match="scale"):
+        mp.KVCache.from_tensors(c.k, c.v, **{"v_scale" if missing == "k_scale" else "k_scale": s})
+    again = mp.KVCache.from_tensors(c.k, c.v, c.k_scale, c.v_scale)
+    assert again.kind == kind and again.head_dim == 64
