@@ -16,7 +16,7 @@
 //
 // The matrix cores take bf16 operands, 2^-8 of a probability's value.  Few rows,
 // which the cache's bytes bound, give each as two bf16 numbers (2^-17) and pay
-// for the second product with 0 to 2 % (16 single tokens over 2952: 135.6 us, 136.6
+// for the second product with 0 to 5 % (16 single tokens over 2952: 135.6 us, 136.6
 // so): their error against 64 bits is that of a float32 softmax, 1.68e-3, all of it
 // the output's rounding, where one number gives 2.12e-3.  Prompts, which the matrix
 // cores bound, would pay 37 % (2944 rows: 88 us, 120 so) for 1.65e-3 in place of
@@ -134,13 +134,15 @@ __device__ __forceinline__ Blocks visible_blocks(int lo, int hi, int window, int
 // stretch of that run, whatever the sequences' lengths; a tile whose blocks lie in
 // several stretches leaves its sums for the kernel after it to join.  Within a
 // stretch each of the four waves streams every fourth block on its own (no
-// barrier until a tile's end).  Bound: the cache's bytes.  A block's keys and
-// values are loaded a block ahead, straight to registers (16 bytes a lane: keys as
-// the first product's operand, values on their way to LDS), so that each wave
-// always has a block in flight; the matrix products and the softmax (a few hundred
-// clocks a block) hide behind them.  16 single tokens over 2952 of 32 heads in bf16
-// (774 MB): 133 us, 5.8 TB/s; 32 over 4096 to 32768 of 4 heads in 4 bits (315 MB):
-// 72 us, 4.4 TB/s, and 7.5 for the join.
+// barrier until a tile's end).  Bound: the cache's bytes.  A block's keys and values
+// come straight to registers (16 bytes a lane: keys as the first product's operand,
+// values on their way to LDS), one set of them: the next block's loads leave when
+// this one's scores are formed and its values are in LDS, and travel under its softmax
+// and second product.  In between a wave has nothing in flight, which the compute
+// unit's other seven cover in part: better with bf16 pages, whose scores and LDS writes
+// are short (16 single tokens over 2952 of 32 heads, 774 MB: 136.5 us, 5.7 TB/s), than
+// with 4-bit ones, which are widened there (32 over 4096 to 32768 of 4 heads, 315 MB: 75 us,
+// 4.2 TB/s, and 7.5 for the join).
 constexpr int kStepWaves = 4;
 
 template <int DH, bool FP4> struct StepShape {
@@ -214,7 +216,7 @@ struct Stretches {
   }
 };
 
-template <int DH, bool FP4>
+template <int DH, bool FP4>  // (2: the launch counts on two workgroups a compute unit)
 __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const CacheAttnArgs a) {
   using X = StepShape<DH, FP4>;
   constexpr int KB = X::KB, NT = X::NT, NM = X::NM, ND = X::ND, NS = X::NS, NV = X::NV;
@@ -653,8 +655,8 @@ namespace {
 // workgroup's rows.  A wave brings the 16 tokens that one table entry names.
 // Bound: the clock, which a full card lowers to 1.6 GHz; a block takes a wave 3600
 // clocks, 1024 of them matrix instructions, 880 the issue of its loads, and the two
-// waves of a SIMD overlap in part.  2944 rows of 32 heads, causal: 88 us (71 GFLOP of
-// visible scores, 0.81 PFLOP/s); two prompts of 4700 rows, 28 heads over 4 in 4 bits,
+// waves of a SIMD overlap in part.  2944 rows of 32 heads, causal: 89 us (71 GFLOP of
+// visible scores, 0.80 PFLOP/s); two prompts of 4700 rows, 28 heads over 4 in 4 bits,
 // window 1152: 206 us (0.69 PFLOP/s).  64 rows a wave, one wave a SIMD: 143 for 89 us.
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 constexpr int kKeys = 64;
@@ -1025,22 +1027,39 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 
 // Sequences of up to so many new rows run on the kernel for few rows: its tiles
 // of 16 (row, head) pairs read the cache once each, n G / 16 times a key/value
-// head, the other kernel once for each of the G heads.
+// head, the other kernel once for each of the G heads, with a quarter of its waves
+// at work up to 32 rows.  Behind 8000 tokens, few rows' kernel / prompts' (us):
+//   rows                       2         8         16         32         64
+//   32 heads over 32        35 / 33   37 / 34   38 / 35    45 / 35    67 / 39
+//   28 heads over 4         27 / 31   33 / 31   37 / 32    49 / 32    68 / 37
+//   8 sequences of these          (4: 45 / 137)  143 / 138  206 / 139  343 / 147
+// and behind 300 tokens, 32 over 32: 10 / 13 at 4 and at 16 rows, 10 / 16 at 32.  The
+// two cross between 8 and 24 rows in all but that short one.
 constexpr int kStepRows = 16;
-
 
 }  // namespace
 
 // The few rows' workgroups: two a compute unit hold the card, each with an equal
-// stretch; fewer where the longest table gives a stretch under eight blocks or a
-// tile over 64 pieces.  Without stretches (0: a workgroup a tile, and no second
-// launch) where no row sees over 512 tokens, or where there is a tile for each place
-// on the card: 16 single tokens over 2952 of 32 heads take 133 us that way and 141 in
-// stretches, whose tiles' ends and second launch cost what the balance does not bring
-// back unless the lengths differ (and where the run might pass 2^30 blocks, which are
-// counted in an int; a window may bring it back, so the workspace has the room).
+// stretch; fewer where the longest table gives a stretch under eight blocks (4, 8 and 16:
+// 16.5, 16.5, 17.6 us for a token of 28 heads over 4 behind 600, 24.9, 25.1, 24.1 for 8
+// behind 3000) or a tile over 64 pieces (32, 64 and 128: 36, 41, 52 us behind 30000, 92,
+// 74, 94 behind 120000).  Without stretches (0: a workgroup a tile, and no second launch)
+//   where no row sees over 512 tokens (one token of 32 heads behind 250, 500, 700, 1000
+//   and 2000: 10.3, 11.4, 14.2, 18.5, 33.2 us in tiles, 13.0, 13.6, 17.1, 14.6, 19.2 in
+//   stretches);
+//   where there is a tile for each place on the card.  That is the better one for
+//   lengths that are alike and for many tiles (16 single tokens over 3000 of 32 heads
+//   139 us in tiles, 143 in stretches; 128 over 100 to 2000: 368 and 428; 256 over 3000 of 8
+//   heads of 64 in 4 bits: 118 and 142), and the worse one just past a full round (17 over
+//   2000 of 32 heads: 125 and 109) and for one sequence far longer than the rest, whose
+//   tiles then run alone (64 sequences of 8 heads, 63 of 200 tokens and one of 32768: 590
+//   and 68).  The lengths are on the device, so the host takes the common case;
+//   and where the run might pass 2^30 blocks, which are counted in an int (a window may
+//   bring it back, so the workspace has the room).
 // Prompts: two workgroups a compute unit, by splitting the tokens where there are
-// fewer tiles, 512 tokens a part at least.
+// fewer tiles, 512 tokens a part at least (256, 512 and 1024: 24.6, 23.5, 36.7 us for 40
+// rows of 32 heads behind 2500, 30.3, 28.7, 41.3 for 500 of 8 behind 2000; 18.7, 25.8,
+// 25.8 for 40 of 8 behind 800).
 // tokens: the most that a row can see.
 CacheAttnPlan cache_attention_plan(const int* off, int B, int Hq, int Hkv, int Dh, bool fp4, long long tokens, int cus) {
   CacheAttnPlan p{};
