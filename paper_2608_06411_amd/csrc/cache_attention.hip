@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheJoinA
     if (b + s < a.prompts && a.prompt[b + s].x <= i) b += s;
   const int r = a.prompt[b].y + i - a.prompt[b].x;
   float mm = kLow, low = 0.0f, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // low: the least l
-  // (a few parts' loads together; past the last, that one's again, at no weight)
+  // (a few parts' loads together; past the last, that one's again, unused)
   for (int s0 = 0; s0 < a.parts; s0 += 4) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -632,12 +632,13 @@ __global__ __launch_bounds__(256) void cache_prompt_join_kernel(const CacheJoinA
       const long long at = (long long)min(s0 + u, a.parts - 1) * items + item;
       const float2 ml = a.part_ml[at];
       const float4 o = *reinterpret_cast<const float4*>(a.part_o + at * DH + d0);
-      const float f = s0 + u < a.parts ? piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-7f) : 0.0f;
-      sum = fmaf(f, fabsf(ml.y), sum);
-      v[0] = fmaf(f, o.x, v[0]);
-      v[1] = fmaf(f, o.y, v[1]);
-      v[2] = fmaf(f, o.z, v[2]);
-      v[3] = fmaf(f, o.w, v[3]);
+      const bool in = s0 + u < a.parts;
+      const float f = piece_weight(ml.x, ml.y, mm, low < 0.0f, 0x1p-7f);
+      sum = in ? fmaf(f, fabsf(ml.y), sum) : sum;
+      v[0] = in ? fmaf(f, o.x, v[0]) : v[0];  // (no weight of zero: the sums may be infinite)
+      v[1] = in ? fmaf(f, o.y, v[1]) : v[1];
+      v[2] = in ? fmaf(f, o.z, v[2]) : v[2];
+      v[3] = in ? fmaf(f, o.w, v[3]) : v[3];
     }
   }
   write_row<4>(static_cast<bf16_t*>(a.out) + r * a.ldo + h * DH + d0, v, sum);

@@ -233,3 +233,25 @@ def test_norms_of_zero_and_of_what_is_not_finite():
     same = torch.ones(4, 6, dtype=torch.bool)
     same[0, 1] = same[2, 3] = same[3, 0] = False
     assert torch.equal(got[same], clean[same])
+
+
+@pytest.mark.parametrize("form", list(FORMS) + ["three parts", "five parts"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_visible_infinity_is_the_rows_value(form, sign):
+    """An infinite value in the last row's own token, among equal scores: that
+    row's channel is infinite, whatever waves, stretches and parts join."""
+    announce(f"a visible infinity, {form}, {sign}")
+    n, past = FORMS.get(form) or ([40], [1700 if form == "three parts" else 2700])
+    b = Held("bf16", 128, 2, 16, n, past, seed=12)
+
+    def values(s, length):
+        v = b.rows(length)
+        if s == 0:
+            v[length - 1, 1, 77] = sign * float("inf")
+        return v
+
+    _store(b, lambda s, length: torch.zeros(length, 2, 128).bfloat16(), values)
+    got = b.attend(b.rows(b.off[-1], heads=4)).cpu()
+    bad = torch.zeros(got.shape, dtype=torch.bool)
+    bad[n[0] - 1, 2:, 77] = True
+    assert (got[bad] == sign * float("inf")).all() and torch.isfinite(got[~bad]).all()
