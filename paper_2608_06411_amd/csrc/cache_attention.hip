@@ -478,11 +478,11 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void cache_step_kernel(const Ca
     }
   }
   };
-  // Every value taken as finite; if a sum comes out infinite or NaN (or a score is far:
-  // far_scores), once more with
-  // smaller probabilities (kShrink), and keeping such values from the rows that
-  // do not see them (their zero probability would not cancel them): the product runs on
-  // the finite values, the others add themselves to the rows that see them.
+  // Every value taken as finite; if a sum comes out infinite or NaN, or a row's scores
+  // are far (far_scores), once more with smaller probabilities (kShrink), keeping such
+  // values from the rows that do not see them (their zero probability would not cancel
+  // them): the product runs on the finite values, the others add themselves to the rows
+  // that see them.
   run(std::false_type{});
   auto sum_l = [&]() {
     l += __shfl_xor(l, 16, 64);
@@ -853,6 +853,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
         for (int r = 0; r < 16; ++r) sc[r] = visible(cur, any, acc_row(r, lane)) ? sc[r] : -INFINITY;
       }
     }
+    // (The half before's, up here, where they are long there: 2944 rows 87.1 us and two
+    // video prompts 202.3; summed right behind their exponentials, 88.3 and 204.9; the
+    // unrounded ones, 86.2 and 200.2, on that card.)
     l = add_weights(before[1], add_weights(before[0], l));
     float mx = sc[0];
 #pragma unroll
@@ -864,14 +867,13 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
 
     scores(i + 1, next);  // (behind the last half: unused)
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         float e = __builtin_amdgcn_exp2f(fmaf(sc[8 * st + k], c2, -m));
         if constexpr (careful.value) e = kShrink * (apart ? __builtin_amdgcn_exp2f(exponent_apart(sc[8 * st + k], c2, m)) : e);
         p[st][k] = static_cast<__bf16>(e);
       }
-    }
     const char* V = lds + (2 + (((i - 1) >> 1) & 1)) * BUF + 32 * ((i - 1) & 1) * ROW;
     auto vfrag = [&](int st, int d) {  // keys 16 st + 4 lh + (0..3) and + 8, value 32 d + lr
       const char* at = V + (16 * st + tr_key) * ROW + 8 * (lane & 3);
@@ -912,11 +914,11 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(const CacheAttnArg
   // Keys of block j are read in steps 2 j - 1 and 2 j, its values in steps 2 j + 1
   // and 2 j + 2: so one meeting a block, before an odd step, that brings the keys of
   // the block after next and the values of the next.
-  // A first run takes every value as finite; if a sum comes out infinite or NaN, or a score
-  // is far (far_scores), a
-  // second one has smaller probabilities (kShrink) and keeps such values from the rows
-  // that do not see them (their zero probability would not cancel them): the product
-  // runs on the finite values, and the others add themselves to the rows that see them.
+  // A first run takes every value as finite; if a sum comes out infinite or NaN, or a
+  // row's scores are far (far_scores), a second one has smaller probabilities (kShrink)
+  // and keeps such values from the rows that do not see them (their zero probability
+  // would not cancel them): the product runs on the finite values, and the others add
+  // themselves to the rows that see them.
   auto run = [&](auto careful) {
 #pragma unroll
     for (int d = 0; d < ND; ++d)
